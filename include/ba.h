@@ -8,6 +8,9 @@
  *   (b) the final block attending every cached block + itself Section 2.5, step 3
  *   (c) block-diagonal prefill of all blocks in one launch    Section 1; Section 2.4
  *
+ * what comes before and after them -- norms and rotation of the projections (with
+ * gradients), appending to a paged cache, attention of a batch that shares a
+ * prefix --
  * plus the integer tables that describe a ragged prompt (Section 2.2, 2.5) and a
  * flag that switches the same entry points to ordinary full causal attention
  * (Section 3: the fine-tuned model runs under either mask).
@@ -413,6 +416,94 @@ ba_status ba_final_attend_fused_paged(ba_ctx *ctx, const void *q_f, const void *
                                       const ba_page_table *pages, int32_t n_cache_rows, void *k_out,
                                       void *o, float *lse, const ba_segments *seg, ba_mode mode,
                                       ba_out_dtype out_dtype, void *stream);
+
+/*
+ * Norms of queries and keys for each head, and the position rotation (Section 2.3, Eq. 1), in one pass: what a layer's projections
+ * need before ba_block_prefill or ba_final_attend take them.  For every row and head
+ *     y = R(pos) (x r w),   r = 1 / sqrt(mean(x^2) + eps),   mean over the head's head_dim values,
+ * in fp32 (angles in fp64), rounded once.
+ *   q, k         bf16 rows of [n_q_heads, head_dim] and [n_kv_heads, head_dim], `q_stride` and `k_stride` elements apart (0: packed; else
+ *                a multiple of 8, not less than a row), so that both may lie in the one buffer of a fused projection.  Either may be
+ *                NULL with its output: that side is left out.
+ *   pos          device int32 [n_rows], any value, or NULL: position 0 throughout, which rotates nothing
+ *   w_q, w_k     bf16 [head_dim], 16-byte aligned, shared by the heads; NULL: that side is rotated only
+ *   eps          not negative; ignored when both weights are NULL
+ *   q_out, k_out bf16 packed [n_rows, heads, head_dim]; may be q, k themselves where those are packed, must not overlap them otherwise
+ */
+ba_status ba_qk_norm_rope(ba_ctx *ctx, const void *q, int64_t q_stride, const void *k, int64_t k_stride, int32_t n_rows,
+                          const int32_t *pos, const void *w_q, const void *w_k, float eps, void *q_out, void *k_out, void *stream);
+
+/*
+ * Gradients of ba_qk_norm_rope.  With g = R(-pos) dy and h = g w:
+ *     dx = r h - x r^3 mean(h x),   dw = sum over rows and heads of g x r;   without a norm dx = g.
+ *   q, k, pos, w_q, w_k, eps   what the forward call was given (q, k are not read, and may be NULL, where there is no norm)
+ *   dy_q, dy_k   packed [n_rows, heads, head_dim]: gradients with respect to q_out, k_out (the dq, dk of ba_block_prefill_bwd); NULL
+ *                with its output: that side is left out
+ *   dq, dk       rows `dq_stride`, `dk_stride` elements apart (0: packed; else a multiple of 16 bytes); may be dy_q, dy_k themselves where packed
+ *   dw_q, dw_k   fp32 [head_dim], written (not added to); given exactly where w_q, w_k are.  Zero for n_rows = 0.
+ *   grad_dtype   type of dy_q, dy_k, dq and dk
+ * Uses 592 * 8 * head_dim bytes of workspace when there is a norm.  No atomics: results are run-to-run identical.
+ */
+ba_status ba_qk_norm_rope_bwd(ba_ctx *ctx, const void *q, int64_t q_stride, const void *k, int64_t k_stride, int32_t n_rows,
+                              const int32_t *pos, const void *w_q, const void *w_k, float eps, const void *dy_q, const void *dy_k,
+                              void *dq, int64_t dq_stride, void *dk, int64_t dk_stride, float *dw_q, float *dw_k,
+                              ba_out_dtype grad_dtype, void *stream);
+
+/*
+ * Section 2.5, after the prompt: keys and values of new tokens go into a paged cache, the keys normed and rotated on the way, and the
+ * queries of the same tokens may ride along (one launch between a decode step's projections and its attention).  Also brings
+ * passages into pages: cached keys (positions 0 .. L - 1) with pos = the block's delta and no norm are re-encoded by Eq. 3.
+ *   q .. eps     as for ba_qk_norm_rope; v, v_stride: the values, laid out like k, copied bit for bit.  q and q_out may be NULL.
+ *   seq_cu       device int32 [n_seqs + 1]: rows seq_cu[s] .. seq_cu[s + 1] - 1 belong to sequence s, not decreasing; NULL: one row each
+ *                (n_seqs = n_rows, else BA_ERR_SHAPE).  Rows outside all sequences (padding) are left alone in every output.
+ *   seq_start    device int32 [n_seqs]: the place in list s of pages that the sequence's first row goes to (its rows so far)
+ *   pages        lists page_cu[s] .. of the sequences in the pools (ba_page_table, with sequences for blocks)
+ *   k_pool, v_pool  bf16 [n_pages * page_rows, n_kv_heads, head_dim]; q, k, v do not overlap them
+ * A row whose place has no page in its list, or a page outside the pool, is not written to the pools and reported through
+ * ba_last_device_status() as BA_ERR_INVALID_ARG; its query is still written.  Two rows must not go to the same place.
+ */
+ba_status ba_append_paged(ba_ctx *ctx, const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                          int32_t n_rows, const int32_t *pos, const void *w_q, const void *w_k, float eps, const int32_t *seq_cu,
+                          const int32_t *seq_start, int32_t n_seqs, void *q_out, void *k_pool, void *v_pool, const ba_page_table *pages,
+                          void *stream);
+
+/*
+ * A batch of sequences in which groups share a prefix (the same passages under different questions; a system prompt).  All tables are on
+ * the device and are read when the kernels run, so that a captured launch follows them.  Sequences of a group are neighbours.
+ */
+typedef struct {
+  int32_t batch;             /* sequences */
+  int32_t n_groups;          /* prefixes; 0: there are none */
+  const int32_t *group_cu;   /* [n_groups + 1] sequences group_cu[g] .. group_cu[g + 1] - 1 share prefix g; sequences outside have none.
+                              * NULL: one group of the whole batch (n_groups = 1) */
+  const int32_t *prefix_cu;  /* [n_groups + 1] prefix g has prefix_cu[g + 1] - prefix_cu[g] rows (ba_segments.cu_cache_seq of the prompts) */
+  const int32_t *q_cu;       /* [batch + 1] query rows of every sequence; NULL: one each */
+  const int32_t *own_len;    /* [batch] rows in the sequence's own cache, its query rows' keys among them */
+} ba_shared_batch;
+
+/*
+ * Attention of such a batch, a prefix read once for all of its group: query row i of the n rows of sequence s sees the whole prefix of
+ * its group and the first own_len[s] - (n - 1 - i) rows of its own cache (the last row sees all of them, as in decoding and after a
+ * question of n tokens).  A row that sees no key gets zeros, and -infinity as its log-sum-exp.
+ *   q            bf16 [n_q_rows, n_q_heads, head_dim], RoPE at prompt positions; rows outside all sequences are left alone in o and lse
+ *   k_prefix, v_prefix   the prefixes, keys at their positions.  prefix_pages NULL: packed [n_prefix_rows, n_kv_heads, head_dim], prefix g
+ *                from row prefix_cu[g] (the k_out of ba_final_attend_fused or the k_dst of ba_reencode_k, beside the cached values);
+ *                else pools of that table, prefix g on list g (n_prefix_rows is not used)
+ *   k_pool, v_pool, pages   the sequences' own rows, sequence s on list s (ba_append_paged fills them); may be the prefixes' pools
+ *   o            [n_q_rows, n_q_heads, head_dim] bf16 or fp32; lse fp32 [n_q_rows, n_q_heads] or NULL
+ * What lies behind the end of a prefix, a sequence or a list in pages or rows is never used and may hold any bits.  A page number outside
+ * its pool counts as zeros and is reported (BA_ERR_INVALID_ARG).  Tables that do not fit together (a cumulative table that decreases
+ * or leaves its range, a length below zero or above its list's pages) are reported the same way and nothing is written.
+ * Uses ba_shared_prefix_bytes() bytes of workspace at most (to be given to ba_create(); BA_ERR_WORKSPACE otherwise); batch + n_groups is
+ * at most BA_SHARED_MAX (BA_ERR_UNSUPPORTED).  No atomics: results are run-to-run identical.
+ */
+#define BA_SHARED_MAX 2048
+ba_status ba_shared_prefix_attend(ba_ctx *ctx, const void *q, int32_t n_q_rows, const void *k_prefix, const void *v_prefix,
+                                  int32_t n_prefix_rows, const ba_page_table *prefix_pages, const void *k_pool, const void *v_pool,
+                                  const ba_page_table *pages, const ba_shared_batch *shared, void *o, float *lse,
+                                  ba_out_dtype out_dtype, void *stream);
+/* Workspace ba_create() should be given for ba_shared_prefix_attend calls of at most these sizes. */
+ba_status ba_shared_prefix_bytes(const ba_config *cfg, int32_t batch, int32_t n_groups, int32_t n_q_rows, size_t *bytes);
 
 #ifdef __cplusplus
 }

@@ -29,8 +29,10 @@ EXPORTS = [
     "ba_final_attend", "ba_reencode_k_noalloc", "ba_selftest_wait_expiry", "ba_reencode_k_deferred", "ba_flush",
     "ba_final_attend_fused", "ba_reencode_k_paged", "ba_final_attend_paged", "ba_final_attend_fused_paged",
     "ba_block_prefill_bwd", "ba_last_attend_shape", "ba_plan_final_attend",
+    "ba_qk_norm_rope", "ba_qk_norm_rope_bwd", "ba_append_paged", "ba_shared_prefix_attend", "ba_shared_prefix_bytes",
 ]
 BA_NOALLOC_MAX_BLOCKS = 4096
+BA_SHARED_MAX = 2048
 
 
 class ba_config(C.Structure):
@@ -60,6 +62,16 @@ class ba_page_table(C.Structure):
 def make_page_table(page_rows: int, n_pages: int, page_cu, page_idx) -> "ba_page_table":
     """page_cu / page_idx: torch int32 CUDA tensors (kept alive by the caller)."""
     return ba_page_table(page_rows, n_pages, _ptr(page_cu), _ptr(page_idx))
+
+
+class ba_shared_batch(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("n_groups", C.c_int32), ("group_cu", C.c_void_p), ("prefix_cu", C.c_void_p),
+                ("q_cu", C.c_void_p), ("own_len", C.c_void_p)]
+
+
+def make_shared_batch(batch: int, n_groups: int, group_cu, prefix_cu, q_cu, own_len) -> "ba_shared_batch":
+    """group_cu / prefix_cu / q_cu / own_len: torch int32 CUDA tensors (kept alive by the caller) or None (see include/ba.h)."""
+    return ba_shared_batch(batch, n_groups, _ptr(group_cu), _ptr(prefix_cu), _ptr(q_cu), _ptr(own_len))
 
 
 class BaError(RuntimeError):
@@ -123,6 +135,12 @@ def _open_library(path: Optional[str]):
     lib.ba_final_attend_fused_paged.argtypes = [vp, vp, vp, vp, i32, vp, vp, pt, i32, vp, vp, vp,
                                                 C.POINTER(ba_segments), C.c_int, C.c_int, vp]
     lib.ba_block_prefill_bwd.argtypes = [vp] + [vp] * 9 + [C.POINTER(ba_segments), C.c_int, C.c_int, vp]
+    i64, f32 = C.c_int64, C.c_float
+    lib.ba_qk_norm_rope.argtypes = [vp, vp, i64, vp, i64, i32, vp, vp, vp, f32, vp, vp, vp]
+    lib.ba_qk_norm_rope_bwd.argtypes = [vp, vp, i64, vp, i64, i32, vp, vp, vp, f32, vp, vp, vp, i64, vp, i64, vp, vp, C.c_int, vp]
+    lib.ba_append_paged.argtypes = [vp, vp, i64, vp, i64, vp, i64, i32, vp, vp, vp, f32, vp, vp, i32, vp, vp, vp, pt, vp]
+    lib.ba_shared_prefix_attend.argtypes = [vp, vp, i32, vp, vp, i32, pt, vp, vp, pt, C.POINTER(ba_shared_batch), vp, vp, C.c_int, vp]
+    lib.ba_shared_prefix_bytes.argtypes = [C.POINTER(ba_config), i32, i32, i32, C.POINTER(sz)]
     for name in EXPORTS:
         # without argtypes ctypes would pass addresses as 32-bit ints
         if getattr(lib, name).argtypes is None:
@@ -131,7 +149,7 @@ def _open_library(path: Optional[str]):
             getattr(lib, name).restype = C.c_int
     marshal = _load_marshal()
     if marshal is not None:
-        marshal.bind(lib._handle, _through_ctypes, vp, ba_segments, ba_page_table)
+        marshal.bind(lib._handle, _through_ctypes, vp, ba_segments, ba_page_table, ba_shared_batch)
     else:
         marshal = _CtypesCalls()
     return lib, marshal
@@ -151,12 +169,15 @@ def _load_marshal():
         return None
 
 
+_MAY_BE_NULL = {("ba_shared_prefix_attend", 6)}      # structures a call can do without: packed prefixes have no pages
+
+
 def _through_ctypes(name, *args):
     """A hot call whose arguments the extension does not take: through ctypes, like every other function of the library."""
     fn = getattr(load_library(), name)
     given = [args[0]]
     for a, t in zip(args[1:], fn.argtypes[1:]):
-        given.append(_ptr(a) if t is C.c_void_p else C.byref(a) if issubclass(t, C._Pointer) else a)
+        given.append(_ptr(a) if t is C.c_void_p else C.byref(a) if issubclass(t, C._Pointer) and not (a is None and (name, len(given)) in _MAY_BE_NULL) else a)
     return fn(*given)
 
 
@@ -344,3 +365,54 @@ def ba_final_attend_fused_paged(ctx, q_f, k_f, v_f, n_final_rows, k_pool, v_pool
 def ba_block_prefill_bwd(ctx, q, k, v, o, lse, d_o, dq, dk, dv, seg, mode, grad_dtype, stream=None):
     _check(_calls().block_prefill_bwd(ctx, q, k, v, o, lse, d_o, dq, dk, dv, seg, mode, grad_dtype, _stream_ptr(stream)),
            "ba_block_prefill_bwd")
+
+
+def ba_shared_prefix_bytes(cfg: ba_config, batch: int, n_groups: int, n_q_rows: int) -> int:
+    out = C.c_size_t(0)
+    _check(load_library().ba_shared_prefix_bytes(C.byref(cfg), batch, n_groups, n_q_rows, C.byref(out)), "ba_shared_prefix_bytes")
+    return out.value
+
+
+def _rows(t, what: str):
+    """Address and row stride of a [rows, heads, head_dim] tensor whose rows may lie apart (a view of a fused projection)."""
+    if t is None or isinstance(t, int):
+        return t, 0
+    if t.is_contiguous():
+        return t.data_ptr(), 0
+    if t.dim() != 3 or t.stride(2) != 1 or t.stride(1) != t.shape[2]:
+        raise ValueError(f"{what}: the heads of a row must lie side by side")
+    return t.data_ptr(), t.stride(0)
+
+
+def ba_qk_norm_rope(ctx, q, k, n_rows, pos, w_q, w_k, eps, q_out, k_out, stream=None):
+    """q, k: [n_rows, heads, head_dim], rows may lie apart (views of a fused projection); None leaves a side out."""
+    q, q_stride = _rows(q, "q")
+    k, k_stride = _rows(k, "k")
+    _check(_calls().qk_norm_rope(ctx, q, q_stride, k, k_stride, n_rows, pos, w_q, w_k, eps, q_out, k_out, _stream_ptr(stream)),
+           "ba_qk_norm_rope")
+
+
+def ba_qk_norm_rope_bwd(ctx, q, k, n_rows, pos, w_q, w_k, eps, dy_q, dy_k, dq, dk, dw_q, dw_k, grad_dtype, stream=None):
+    """q, k, dq, dk: rows may lie apart; dw_q, dw_k: fp32 [head_dim], overwritten."""
+    q, q_stride = _rows(q, "q")
+    k, k_stride = _rows(k, "k")
+    dq, dq_stride = _rows(dq, "dq")
+    dk, dk_stride = _rows(dk, "dk")
+    _check(_calls().qk_norm_rope_bwd(ctx, q, q_stride, k, k_stride, n_rows, pos, w_q, w_k, eps, dy_q, dy_k, dq, dq_stride, dk, dk_stride,
+                                     dw_q, dw_k, grad_dtype, _stream_ptr(stream)), "ba_qk_norm_rope_bwd")
+
+
+def ba_append_paged(ctx, q, k, v, n_rows, pos, w_q, w_k, eps, seq_cu, seq_start, n_seqs, q_out, k_pool, v_pool, pages, stream=None):
+    """q (or None), k, v: rows may lie apart; seq_cu None: one row a sequence."""
+    q, q_stride = _rows(q, "q")
+    k, k_stride = _rows(k, "k")
+    v, v_stride = _rows(v, "v")
+    _check(_calls().append_paged(ctx, q, q_stride, k, k_stride, v, v_stride, n_rows, pos, w_q, w_k, eps, seq_cu, seq_start, n_seqs, q_out,
+                                 k_pool, v_pool, pages, _stream_ptr(stream)), "ba_append_paged")
+
+
+def ba_shared_prefix_attend(ctx, q, n_q_rows, k_prefix, v_prefix, n_prefix_rows, prefix_pages, k_pool, v_pool, pages, shared, o, lse,
+                            out_dtype, stream=None):
+    """prefix_pages: ba_page_table or None (packed prefixes); shared: make_shared_batch()."""
+    _check(_calls().shared_prefix_attend(ctx, q, n_q_rows, k_prefix, v_prefix, n_prefix_rows, prefix_pages, k_pool, v_pool, pages, shared, o,
+                                         lse, out_dtype, _stream_ptr(stream)), "ba_shared_prefix_attend")

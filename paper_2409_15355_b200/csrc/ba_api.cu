@@ -10,6 +10,7 @@ ba_status ba_attend_sm100_launch(ba_ctx *ctx, const ba_attend_args &a, const ba_
                                  cudaStream_t stream);
 ba_status ba_attend_sm100_setup(ba_ctx *ctx);
 ba_status ba_bwd_sm100_setup(ba_ctx *ctx);
+ba_status ba_shared_sm100_setup();
 ba_status ba_bwd_sm100_launch(ba_ctx *ctx, const void *q, const void *k, const void *v, const void *o,
                               const float *lse, const void *d_o, void *dq, void *dk, void *dv, int out_f32,
                               const ba_segments *seg, int mode, cudaStream_t stream);
@@ -107,8 +108,11 @@ ba_status ba_workspace_bytes(const ba_config *cfg, int32_t max_blocks, int32_t m
   if (stage < 64 * 1024) stage = 64 * 1024;
   // the backward pass keeps dO . O (fp32 per row and query head) there
   size_t bwd = (size_t)max_q_rows * cfg->n_q_heads * sizeof(float);
+  // gradients of the norms' weights: sums of every CTA
+  const size_t norms = (size_t)kBaNormGridMax * 2 * cfg->head_dim * sizeof(float);
   size_t scratch = table > splits ? table : splits;
   if (bwd > scratch) scratch = bwd;
+  if (norms > scratch) scratch = norms;
   *bytes = stage + ba_align_up(scratch, 256) + 256;
   return BA_OK;
 }
@@ -149,7 +153,7 @@ ba_status ba_create(ba_ctx **out, const ba_config *cfg, int device, size_t works
       // launch counters of the attention kernels (below the scratch area): zero once, every launch leaves them zero
       (workspace_bytes >= ba_scratch_offset(ctx) &&
        cudaMemset(ba_counters(ctx), 0, 256) != cudaSuccess) ||
-      ba_attend_sm100_setup(ctx) != BA_OK || ba_bwd_sm100_setup(ctx) != BA_OK) {
+      ba_attend_sm100_setup(ctx) != BA_OK || ba_bwd_sm100_setup(ctx) != BA_OK || ba_shared_sm100_setup() != BA_OK) {
     cudaGetLastError();
     ba_attend_sm100_teardown(ctx);
     if (ctx->workspace) cudaFree(ctx->workspace);
@@ -500,17 +504,21 @@ ba_status ba_block_prefill_bwd(ba_ctx *ctx, const void *q, const void *k, const 
                              (cudaStream_t)stream);
 }
 
-static ba_status check_pages(const ba_page_table *pg) {
+}  // extern "C"
+
+ba_status ba_check_pages(const ba_page_table *pg) {
   if (!pg || !pg->page_cu || !pg->page_idx) return BA_ERR_INVALID_ARG;
   if (pg->page_rows < 16 || pg->page_rows > 65536 || (pg->page_rows & (pg->page_rows - 1))) return BA_ERR_UNSUPPORTED;
   if (pg->n_pages < 1 || (long long)pg->n_pages * pg->page_rows > 0x7fffffffLL) return BA_ERR_INVALID_ARG;
   return BA_OK;
 }
 
+extern "C" {
+
 ba_status ba_reencode_k_paged(ba_ctx *ctx, const void *k_pool, const ba_page_table *pages, void *k_dst,
                               const int32_t *cu, const int32_t *delta, int32_t n_blocks, int32_t n_rows,
                               void *stream) {
-  ba_status st = check_pages(pages);
+  ba_status st = ba_check_pages(pages);
   if (st != BA_OK) return st;
   const int32_t n_src_rows = pages->n_pages * pages->page_rows;
   bool nothing;
@@ -546,7 +554,7 @@ ba_status ba_final_attend_paged(ba_ctx *ctx, const void *q_f, const void *k_f, c
   ba_attend_args a;
   memset(&a, 0, sizeof(a));
   if (n_cache_rows > 0) {
-    st = check_pages(pages);
+    st = ba_check_pages(pages);
     if (st != BA_OK) return st;
     if (!k_cache || !v_pool || !aligned16(k_cache) || !aligned16(v_pool) || !seg->cache_tile_cu) return BA_ERR_INVALID_ARG;
     a.page_rows = pages->page_rows; a.page_cu = pages->page_cu; a.page_idx = pages->page_idx;
@@ -574,7 +582,7 @@ ba_status ba_final_attend_fused_paged(ba_ctx *ctx, const void *q_f, const void *
   ba_attend_args a;
   memset(&a, 0, sizeof(a));
   if (n_cache_rows > 0) {
-    st = check_pages(pages);
+    st = ba_check_pages(pages);
     if (st != BA_OK) return st;
     if (!k_pool || !v_pool || !aligned16(k_pool) || !aligned16(v_pool)) return BA_ERR_INVALID_ARG;
     if (!seg->cache_rope || !seg->cache_tile_cu) return BA_ERR_INVALID_ARG;

@@ -1717,6 +1717,11 @@ constexpr int attend_smem_bytes() {
 
 }  // namespace
 
+// The same for the library's other kernels.
+bool ba_tensor_map(ba_ctx *ctx, CUtensorMap *out, const void *ptr, int heads, long long rows, int box_heads, int box_rows) {
+  return cached_map(ctx, out, ptr, ctx->cfg.head_dim, heads, rows, box_heads, box_rows);
+}
+
 // Per-context set-up of the attention path, with the context's device current: the kernels' shared-memory
 // limit is raised once here instead of on every launch, and the tensor-map table is created.
 ba_status ba_attend_sm100_setup(ba_ctx *ctx) {

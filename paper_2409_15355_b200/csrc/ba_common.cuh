@@ -169,6 +169,12 @@ ba_reencode_job ba_make_reencode_job(const ba_ctx *ctx, const void *k_src, const
 // Runs a pending deferred job as a stand-alone launch (no-op when nothing is pending).
 ba_status ba_flush_pending(ba_ctx *ctx, cudaStream_t stream);
 
+// Checks of a page table's host-side fields.
+ba_status ba_check_pages(const ba_page_table *pages);
+
+// CTAs whose sums of the norms' weight gradients the workspace has room for (four on each of 148 SMs).
+constexpr int kBaNormGridMax = 592;
+
 struct ba_attend_args {
   // queries / outputs: rows of the q packing (prompt packing for prefill, final packing for final attend)
   const __nv_bfloat16 *q;

@@ -15,7 +15,8 @@
 #include "ba.h"
 
 static PyObject *s_data_ptr, *s_is_contiguous;
-static PyObject *other_way, *t_handle, *t_segments, *t_pages;   /* bind()'s: the ctypes way, c_void_p, ba_segments, ba_page_table */
+static PyObject *other_way, *t_handle, *t_segments, *t_pages, *t_shared;
+/* bind()'s: the ctypes way, c_void_p, ba_segments, ba_page_table, ba_shared_batch */
 
 /* The converters return 1, 0 (an exception is set) or this: not an argument this file takes. */
 #define UNUSUAL (-1)
@@ -77,6 +78,19 @@ static int to_size(PyObject *o, size_t *out) {
   *out = PyLong_AsSize_t(o);
   return *out == (size_t)-1 && PyErr_Occurred() ? unusual_if(PyExc_OverflowError) : 1;
 }
+static int to_int64(PyObject *o, int64_t *out) {
+  if (!PyLong_Check(o)) return UNUSUAL;
+  int overflow;
+  const long long v = PyLong_AsLongLongAndOverflow(o, &overflow);
+  if (overflow) return UNUSUAL;
+  *out = (int64_t)v;
+  return 1;
+}
+static int to_float(PyObject *o, float *out) {
+  if (!PyFloat_Check(o)) return UNUSUAL;
+  *out = (float)PyFloat_AS_DOUBLE(o);
+  return 1;
+}
 /* other_way(name, arguments ...) */
 static PyObject *go_other_way(const char *name, PyObject *const *args, Py_ssize_t nargs) {
   PyObject *all = PyTuple_New(nargs + 1), *n = PyUnicode_FromString(name);
@@ -102,6 +116,9 @@ static PyObject *go_other_way(const char *name, PyObject *const *args, Py_ssize_
 #define CTX ba_ctx *ctx; TAKE(to_context(args[0], &ctx))
 #define SEG(i, v) void *v; TAKE(to_memory(args[i], t_segments, sizeof(ba_segments), &v))
 #define PAGES(i, v) void *v; TAKE(to_memory(args[i], t_pages, sizeof(ba_page_table), &v))
+#define L(i, v) int64_t v; TAKE(to_int64(args[i], &v))
+#define F(i, v) float v; TAKE(to_float(args[i], &v))
+#define SHARED(i, v) void *v; TAKE(to_memory(args[i], t_shared, sizeof(ba_shared_batch), &v))
 #define CALL(expr)                                   \
   do {                                               \
     ba_status st;                                    \
@@ -110,8 +127,11 @@ static PyObject *go_other_way(const char *name, PyObject *const *args, Py_ssize_
   } while (0)
 #define FUNCTIONS(X) X(ba_segment) X(ba_reencode_k) X(ba_reencode_k_paged) X(ba_block_prefill) X(ba_block_prefill_bwd) \
   X(ba_final_attend) X(ba_final_attend_fused) X(ba_final_attend_paged) X(ba_final_attend_fused_paged)
+/* (a library without these is taken as well: calls of them go the ctypes way) */
+#define MORE_FUNCTIONS(X) X(ba_qk_norm_rope) X(ba_qk_norm_rope_bwd) X(ba_append_paged) X(ba_shared_prefix_attend)
 #define DECLARE(f) static __typeof__(&f) p_##f;
 FUNCTIONS(DECLARE)
+MORE_FUNCTIONS(DECLARE)
 
 static PyObject *m_segment(PyObject *self, PyObject *const *args, Py_ssize_t nargs) {
   ARGS(ba_segment, 11); CTX; P(1, lens); P(2, nblocks); I(3, batch); I(4, n_blocks); I(5, n_tokens); I(6, mode); P(7, buf);
@@ -157,19 +177,46 @@ static PyObject *m_final_attend_fused_paged(PyObject *self, PyObject *const *arg
   CALL(p_ba_final_attend_fused_paged(ctx, q, k, v, n_final, kp, vp, pages, n_cache, k_out, o, lse, seg, mode, out, stream));
 }
 
-/* bind(handle, other_way, c_void_p, ba_segments, ba_page_table): take the library's functions from the shared object a dlopen
+#define PRESENT(f) if (!p_##f || !t_shared) return go_other_way(function, args, nargs)
+static PyObject *m_qk_norm_rope(PyObject *self, PyObject *const *args, Py_ssize_t nargs) {
+  ARGS(ba_qk_norm_rope, 13); PRESENT(ba_qk_norm_rope); CTX; P(1, q); L(2, qs); P(3, k); L(4, ks); I(5, n); P(6, pos); P(7, wq); P(8, wk); F(9, eps);
+  P(10, q_out); P(11, k_out); P(12, stream);
+  CALL(p_ba_qk_norm_rope(ctx, q, qs, k, ks, n, pos, wq, wk, eps, q_out, k_out, stream));
+}
+static PyObject *m_qk_norm_rope_bwd(PyObject *self, PyObject *const *args, Py_ssize_t nargs) {
+  ARGS(ba_qk_norm_rope_bwd, 20); PRESENT(ba_qk_norm_rope_bwd); CTX; P(1, q); L(2, qs); P(3, k); L(4, ks); I(5, n); P(6, pos); P(7, wq); P(8, wk);
+  F(9, eps); P(10, dyq); P(11, dyk); P(12, dq); L(13, dqs); P(14, dk); L(15, dks); P(16, dwq); P(17, dwk); I(18, type); P(19, stream);
+  CALL(p_ba_qk_norm_rope_bwd(ctx, q, qs, k, ks, n, pos, wq, wk, eps, dyq, dyk, dq, dqs, dk, dks, dwq, dwk, type, stream));
+}
+static PyObject *m_append_paged(PyObject *self, PyObject *const *args, Py_ssize_t nargs) {
+  ARGS(ba_append_paged, 20); PRESENT(ba_append_paged); CTX; P(1, q); L(2, qs); P(3, k); L(4, ks); P(5, v); L(6, vs); I(7, n); P(8, pos); P(9, wq);
+  P(10, wk); F(11, eps); P(12, cu); P(13, start); I(14, n_seqs); P(15, q_out); P(16, kp); P(17, vp); PAGES(18, pages); P(19, stream);
+  CALL(p_ba_append_paged(ctx, q, qs, k, ks, v, vs, n, pos, wq, wk, eps, cu, start, n_seqs, q_out, kp, vp, pages, stream));
+}
+static PyObject *m_shared_prefix_attend(PyObject *self, PyObject *const *args, Py_ssize_t nargs) {
+  ARGS(ba_shared_prefix_attend, 15); PRESENT(ba_shared_prefix_attend); CTX; P(1, q); I(2, n); P(3, kx); P(4, vx); I(5, nx);
+  void *px = NULL;
+  if (args[6] != Py_None) TAKE(to_memory(args[6], t_pages, sizeof(ba_page_table), &px));
+  P(7, kp); P(8, vp); PAGES(9, pages); SHARED(10, shared); P(11, o); P(12, lse); I(13, out); P(14, stream);
+  CALL(p_ba_shared_prefix_attend(ctx, q, n, kx, vx, nx, px, kp, vp, pages, shared, o, lse, out, stream));
+}
+
+/* bind(handle, other_way, c_void_p, ba_segments, ba_page_table[, ba_shared_batch]): take the library's functions from the shared object a dlopen
  * handle names. */
 static PyObject *m_bind(PyObject *self, PyObject *args) {
-  PyObject *handle, *way, *handle_type, *segments, *pages;
-  if (!PyArg_ParseTuple(args, "OOOOO", &handle, &way, &handle_type, &segments, &pages)) return NULL;
+  PyObject *handle, *way, *handle_type, *segments, *pages, *shared = NULL;
+  if (!PyArg_ParseTuple(args, "OOOOO|O", &handle, &way, &handle_type, &segments, &pages, &shared)) return NULL;
   void *h = PyLong_AsVoidPtr(handle);
   if (!h && PyErr_Occurred()) return NULL;
 #define RESOLVE(f) \
   if (!(p_##f = (__typeof__(&f))dlsym(h, #f))) return PyErr_Format(PyExc_RuntimeError, "%s is not in the library", #f);
   FUNCTIONS(RESOLVE)
+#define RESOLVE_IF_THERE(f) p_##f = (__typeof__(&f))dlsym(h, #f);
+  MORE_FUNCTIONS(RESOLVE_IF_THERE)
   Py_XSETREF(t_handle, Py_NewRef(handle_type));
   Py_XSETREF(t_segments, Py_NewRef(segments));
   Py_XSETREF(t_pages, Py_NewRef(pages));
+  if (shared) Py_XSETREF(t_shared, Py_NewRef(shared));
   Py_XSETREF(other_way, Py_NewRef(way));
   Py_RETURN_NONE;
 }
@@ -177,7 +224,8 @@ static PyObject *m_bind(PyObject *self, PyObject *args) {
 #define METHOD(n) {#n, (PyCFunction)(void (*)(void))m_##n, METH_FASTCALL, NULL}
 static PyMethodDef methods[] = {{"bind", m_bind, METH_VARARGS, NULL}, METHOD(segment), METHOD(reencode_k), METHOD(reencode_k_paged),
                                 METHOD(block_prefill), METHOD(block_prefill_bwd), METHOD(final_attend), METHOD(final_attend_fused),
-                                METHOD(final_attend_paged), METHOD(final_attend_fused_paged), {NULL, NULL, 0, NULL}};
+                                METHOD(final_attend_paged), METHOD(final_attend_fused_paged),
+                                METHOD(qk_norm_rope), METHOD(qk_norm_rope_bwd), METHOD(append_paged), METHOD(shared_prefix_attend), {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "ba_marshal", NULL, -1, methods, NULL, NULL, NULL, NULL};
 PyMODINIT_FUNC PyInit_ba_marshal(void) {
   s_data_ptr = PyUnicode_InternFromString("data_ptr");

@@ -26,11 +26,11 @@ class Context:
     """Owns a ba_ctx.  One per stream."""
 
     def __init__(self, n_q_heads, n_kv_heads, head_dim, rope_theta, rope_layout=B.BA_ROPE_ADJACENT,
-                 softmax_scale=0.0, device=0, max_blocks=4096, max_q_rows=1 << 20):
+                 softmax_scale=0.0, device=0, max_blocks=4096, max_q_rows=1 << 20, workspace_bytes=0):
         self.cfg = B.ba_config(n_q_heads, n_kv_heads, head_dim, rope_layout, float(rope_theta),
                                float(softmax_scale), 0)
         self.device = device
-        ws = B.ba_workspace_bytes(self.cfg, max_blocks, max_q_rows)
+        ws = max(B.ba_workspace_bytes(self.cfg, max_blocks, max_q_rows), workspace_bytes)
         self.ctx = B.ba_create(self.cfg, device, ws)
 
     @classmethod
