@@ -1,20 +1,26 @@
 // Attention of a batch whose sequences share prefixes, over a paged cache (the steps after a prompt).
 //
 // Work.  An entry is a prefix with the query rows of its whole group, or a sequence's own rows with its queries.  The rows of an entry
-// are (token, head of a KV group) pairs, 32 to a row tile; entry x KV head x row tile is an item, its keys come in tiles of 128.  The key
-// tiles of all items, laid end to end, are one stream that is cut into equal runs, one per SM, so that one long sequence, many short
-// ones and a prefix of 32K keep every SM equally long.  The cut pieces of an item leave partial results (normalised rows and their
-// log-sum-exp) that a second kernel merges, prefix and own rows alike; an item that is whole, of a sequence without prefix, is
-// written straight to the output.  The stream is laid out on the device from the caller's tables by every CTA for itself: the lengths
-// of a captured launch change from replay to replay.
+// are (token, head of a KV group) pairs; its keys come in tiles of 128.  Entries are of two kinds, by their rows:
+//   few  (at most 16): a key is used by few rows, the bytes of the cache are all that counts.  An item is entry x KV head.
+//   many (more): a matrix product.  An item is entry x KV head x 256 rows (two tiles of 128), for the tensor core.
+// The key tiles of all items of a kind, laid end to end, are a stream that is cut into equal runs, one per CTA; the CTAs are shared out
+// among the two streams by their cost.  So one long sequence, many short ones and a prefix of 32K keep every SM equally long.
+// An item that a cut divides leaves partial results (normalised rows and their log-sum-exp), in the rows of its queries for its first
+// piece and in a place of the CTA for the others (a run starts with one such piece at most); a second kernel merges them, prefix
+// and own rows alike.  An item of few rows that is whole, of a sequence without prefix, is written straight to the output.  The streams are
+// laid out on the device from the caller's tables by every CTA for itself: the lengths of a captured launch change from replay to replay.
 //
-// Structure of a CTA (384 threads, one per SM): warp 8 asks the copy engine for key and value tiles (a ring of stages, one box per page);
-// warps 0-7 take 16 keys of a tile each.  With few rows a key (a decode step has one token x the heads of a group) everything is bound by
-// the bytes of the cache, so the products need no more than mma.sync on operands from shared memory: S = Q K^T, softmax with
-// maxima and sums of the warp's own keys, O += P V with P from registers.  The warps share nothing until the end of a piece, where
-// their maxima, sums and accumulators are merged through shared memory.
+// A CTA has 384 threads, one CTA runs on an SM.
+// Few rows: warp 8 asks the copy engine for key and value tiles (a ring of stages, one box per page); warps 0-7 take 16 keys of a tile
+// each, with mma.sync on operands from shared memory: S = Q K^T, softmax with maxima and sums of the warp's own keys, O += P V with P from
+// registers.  The warps share nothing until the end of a piece, where their maxima, sums and accumulators are merged.
+// Many rows: tcgen05 with accumulators in tensor memory, warps 0-3 and 4-7 softmax (a thread a row), warp 8 copies, warp 9 issues the
+// products, warps 10-11 fetch queries.  Items of more than 128 rows: the two softmax groups have a tile of queries each and share key
+// tiles; items of fewer: they share the query tile and take key tiles in turn, each with an accumulator of its own, so that products and
+// exponentials overlap there too; the merge counts them as two results.
 //
-// Rounding: P to bf16 (the products' type; 2^-9 relative, the sums of the softmax are taken before it), o once at the end.
+// Rounding: P to bf16 (the products' type; 2^-8 relative at most, the sums of the softmax are taken before it), o once at the end.
 #include <algorithm>
 
 #include "ba_common.cuh"
@@ -27,12 +33,16 @@ bool ba_tensor_map(ba_ctx *ctx, CUtensorMap *out, const void *ptr, int heads, lo
 namespace {
 
 constexpr int kTile = 128;            // keys per tile
-constexpr int kRows = 32;             // rows per row tile
+constexpr int kRows = 16;             // most rows of an entry of few: one tile of mma.sync
+constexpr int kManyRows = 256;        // rows of an item of many
 constexpr int kWarps = 8;             // consumer warps
 constexpr int kThreads = 32 * kWarps + 128;
-// Registers after launch (168 a thread): 256 * 224 + 128 * 56 = 384 * 168.  Two row tiles of 16 keep 128 accumulators and 64 words of queries.
+// Registers after launch (168 a thread): 256 * 224 + 128 * 56 = 384 * 168.  A thread keeps 64 accumulators and 32 words of queries.
 constexpr int kConsumerRegs = 224, kCopyRegs = 56;
 constexpr int kMaxEntries = BA_SHARED_MAX;
+constexpr int kSoftmaxRegs = 208, kServiceRegs = 88;     // of CTAs for many rows: 256 * 208 + 128 * 88
+// What a key tile costs, to share out the CTAs: two query tiles, one, and few rows (cycles / 1000).
+constexpr double kCostPair = 4., kCostSolo = 3., kCostFew = 3.;
 constexpr float kRescale = 8.f;       // O is rescaled when a maximum grows by more than 2^8: exact in real arithmetic, values stay bounded
 
 struct SharedParams {
@@ -48,34 +58,43 @@ struct SharedParams {
   int prefix_paged;
   const int32_t *prefix_page_cu, *prefix_page_idx, *page_cu, *page_idx;
   int prefix_page_lg, page_lg, prefix_pages, n_pages;
-  float *part;                        // partial results: a slot is [kRows][D] values and [kRows] log-sum-exps
-  int n_slots;
-  int4 *meta;                         // [n_groups + batch]: first unit, tiles, row tiles, first item; then one of units a CTA, validity
+  // partial results, normalised: [n_part][D] values, then [n_part] log-sum-exps.  First pieces of items: four arrays indexed as o (own
+  // rows, prefixes, and the second softmax group's share of each); then kManyRows for every CTA.
+  float *part;
+  long long n_part;
+  int4 *meta;                         // [n_groups + batch]: first unit in its stream, tiles, rows, many; then runs of the two kinds, CTAs for many, validity
 };
 
 template <int D>
 struct SharedLayout {
-  static constexpr int kChunks = D / 64;
   static constexpr int kTileBytes = kTile * D * 2;
-  static constexpr int kStages = D == 128 ? 5 : 10;
   static constexpr int kRegion = kTile * 128;
+  // few rows
+  static constexpr int kStages = D == 128 ? 5 : 10;
   static constexpr int kBufStride = 68;                                // floats a row: rows of a quad's lanes in different banks
   static constexpr int kBuf = kStages * kTileBytes;                    // [kWarps][16][kBufStride]
   static constexpr int kStat = kBuf + kWarps * 16 * kBufStride * 4;    // [kWarps][kRows] (maximum, sum)
-  static constexpr int kUnits = kStat + kWarps * kRows * 8;            // [kMaxEntries + 1]
-  static constexpr int kItems = kUnits + (kMaxEntries + 4) * 4;        // [kMaxEntries + 1]
-  static constexpr int kCtrl = kItems + (kMaxEntries + 4) * 4;
-  static constexpr int kBytes = kCtrl + 512 + 1024;
-  static constexpr int kSlot = kRows * (D + 1);                        // floats
+  static constexpr int kFewEnd = kStat + kWarps * kRows * 8;
+  // many rows: query tiles, key tiles, value tiles, write-out
+  static constexpr int kDepth = D == 128 ? 2 : 4;                      // stages of keys, and of values
+  static constexpr int kKeys = 2 * kTileBytes, kValues = kKeys + kDepth * kTileBytes;
+  static constexpr int kOut = kValues + kDepth * kTileBytes;           // [kWarps][32 rows][16 columns]
+  static constexpr int kManyEnd = kOut + kWarps * 32 * 16 * 4;
+  static constexpr int kEnd = kFewEnd > kManyEnd ? kFewEnd : kManyEnd;
+  static constexpr int kUnits = (kEnd + 15) / 16 * 16;                 // [2][kMaxEntries + 4]: units before an entry, by kind
+  static constexpr int kCtrl = kUnits + 2 * (kMaxEntries + 4) * 4;
+  static constexpr int kBytes = kCtrl + 640 + 1024;
 };
 static_assert(SharedLayout<128>::kBytes <= 227 * 1024, "shared memory");
 
 struct SharedCtrl {
-  uint64_t full[10], empty[10];
+  uint64_t full[10], empty[10];       // few: the ring; many: keys [0 .. 3], values [4 .. 7]
+  uint64_t q_full, q_empty, s_full[2], p_full[2][2], o_done[2], o_free[2];
   int abort_flag, invalid;
-  int warp_units[kThreads / 32], warp_items[kThreads / 32];
+  uint32_t tmem_base;
+  double warp_units[2][kThreads / 32], warp_cost[kThreads / 32];
 };
-static_assert(sizeof(SharedCtrl) <= 512, "control area");
+static_assert(sizeof(SharedCtrl) <= 640, "control area");
 
 // An entry, looked up by the thread that asks: rows q_row0 .. of the queries, `len` keys.
 struct Entry { int q_row0, rows, len; };
@@ -110,7 +129,15 @@ __device__ __forceinline__ bool entry_holds(const SharedParams &p, int e) {
   return len == 0 || (long long)len <= ((long long)__ldg(p.page_cu + s + 1) - __ldg(p.page_cu + s)) << p.page_lg;
 }
 __device__ __forceinline__ int tiles_of(const Entry &x) { return (x.len + kTile - 1) / kTile; }
-__device__ __forceinline__ int row_tiles_of(const SharedParams &p, const Entry &x) { return (int)(((long long)x.rows * p.G + kRows - 1) / kRows); }
+__device__ __forceinline__ bool is_many(const SharedParams &p, const Entry &x) { return x.rows * p.G > kRows; }
+__device__ __forceinline__ int row_tiles_of(const SharedParams &p, const Entry &x) { return is_many(p, x) ? (x.rows * p.G + kManyRows - 1) / kManyRows : x.rows > 0; }
+// Index in the partial results of row r of an entry, head h, of an item's first piece: `which` 0 own rows, 1 a prefix, + 2 the second
+// softmax group's.
+__device__ __forceinline__ long long first_part(const SharedParams &p, const Entry &x, int r, int h, int which) {
+  const int tok = r / p.G;
+  return ((long long)which * p.n_q_rows + x.q_row0 + tok) * p.Hq + h * p.G + r - tok * p.G;
+}
+__device__ __forceinline__ long long cut_part(const SharedParams &p, int cta) { return 4ll * p.n_q_rows * p.Hq + (long long)cta * kManyRows; }
 
 // Last index in x[0 .. n] whose value is at most v (x[0] = 0 <= v).
 __device__ __forceinline__ int last_at_most(const int *x, int n, int v) {
@@ -127,23 +154,65 @@ __device__ __forceinline__ int group_of(const SharedParams &p, int s) {
   return lo - 1 < p.n_groups ? lo - 1 : -1;
 }
 
-// A piece of the stream: key tiles tile0 .. tile0 + n - 1 of an item.
+// A piece of a stream: key tiles tile0 .. tile0 + n - 1 of an item, rows row0 .. row0 + n_rows - 1 of its entry.
 struct Piece {
-  int e, head, row_tile, tile0, n, tiles, slot;
+  int e, head, row0, n_rows, tile0, n, tiles;
   Entry x;
 };
 // The piece that starts at unit `at` of this CTA's run, which ends at `end`.
-__device__ __forceinline__ Piece piece_at(const SharedParams &p, const int *units, const int *items, int n_entries, int at, int end) {
+__device__ __forceinline__ Piece piece_at(const SharedParams &p, const int *units, int n_entries, int at, int end) {
   Piece k;
   k.e = last_at_most(units, n_entries, at);
   k.x = get_entry(p, k.e);
   k.tiles = tiles_of(k.x);
   const int local = at - units[k.e], item = local / k.tiles, rts = row_tiles_of(p, k.x);
   k.tile0 = local - item * k.tiles;
-  k.head = item / rts; k.row_tile = item - k.head * rts;
+  k.head = item / rts; k.row0 = (item - k.head * rts) * kManyRows;
+  k.n_rows = min(kManyRows, k.x.rows * p.G - k.row0);
   k.n = min(k.tiles - k.tile0, end - at);
-  k.slot = items[k.e] + item + (int)blockIdx.x;
   return k;
+}
+// Where the keys of a piece lie.  Lane i of the copying warp has box i of a tile, a box per page.
+struct Source {
+  const int32_t *idx;
+  int lg, n_pages, sub_rows, list, first, len;
+  bool paged;
+};
+__device__ __forceinline__ Source source_of(const SharedParams &p, const Piece &k) {
+  const bool own = k.e >= p.n_groups;
+  Source s;
+  s.paged = own || p.prefix_paged;
+  s.lg = own ? p.page_lg : p.prefix_page_lg; s.n_pages = own ? p.n_pages : p.prefix_pages;
+  s.sub_rows = s.paged ? min(kTile, 1 << s.lg) : kTile;
+  s.list = own ? __ldg(p.page_cu + k.e - p.n_groups) : s.paged ? __ldg(p.prefix_page_cu + k.e) : 0;
+  s.idx = own ? p.page_idx : p.prefix_page_idx;
+  s.first = s.paged ? 0 : __ldg(p.prefix_cu + k.e);
+  s.len = k.x.len;
+  return s;
+}
+// First row of this lane's box of a tile; -1: it has none, or nothing lies there.
+__device__ __forceinline__ int box_row(const SharedParams &p, const Source &s, int tile) {
+  const int lane = threadIdx.x & 31, t = tile * kTile + lane * s.sub_rows;
+  if (lane * s.sub_rows >= kTile || t >= s.len) return -1;
+  if (!s.paged) return s.first + t;
+  const int page = __ldg(s.idx + s.list + (t >> s.lg));
+  if (page < 0 || page >= s.n_pages) {
+    ba_record_status(p.status, BA_ERR_INVALID_ARG);
+    return s.n_pages << s.lg;                              // behind the pool: the copy engine fills in zeros
+  }
+  return (page << s.lg) + (t & ((1 << s.lg) - 1));
+}
+// One tile into shared memory, by the whole copying warp.
+template <int D>
+__device__ __forceinline__ void copy_tile(const Source &s, const CUtensorMap *m, uint8_t *dst, uint64_t *bar, int head, int row) {
+  const unsigned boxes = __popc(__ballot_sync(0xffffffffu, row >= 0));
+  if ((threadIdx.x & 31) == 0) mbar_arrive_expect_tx(bar, boxes * s.sub_rows * D * 2);
+  __syncwarp();
+  if (row >= 0) {
+    dst += (threadIdx.x & 31) * s.sub_rows * 128;
+    for (int c = 0; c < D / 64; ++c) tma_load_3d(dst + c * SharedLayout<D>::kRegion, m, bar, c * 64, head, row);
+  }
+  __syncwarp();
 }
 
 __device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
@@ -162,39 +231,33 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 }
 __device__ __forceinline__ void consumers_sync() { asm volatile("bar.sync 1, %0;" ::"n"(32 * kWarps) : "memory"); }
 
-// One piece of an item with kM x 16 rows: the consumer warps' work.  Returns with the ring position moved on.
-template <int D, int kM>
+// One piece of an item of few rows: the consumer warps' work.  Moves the ring position on.
+template <int D>
 __device__ __forceinline__ void consume_piece(const SharedParams &p, const Piece &k, uint8_t *smem, SharedCtrl *ctrl, int &ring, bool &ok, bool direct) {
   using L = SharedLayout<D>;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, quad = lane >> 2, in_quad = lane & 3;
   volatile int *abort_flag = &ctrl->abort_flag;
   const bool own = k.e >= p.n_groups;
-  const int n_rows = min(kRows, k.x.rows * p.G - k.row_tile * kRows);
-  // queries as A operands, straight from memory; rows past the item's are zeros
-  uint32_t qa[kM][D / 16][4];
-  int limit[kM][2];                      // keys that the lane's rows see
+  const int n_rows = k.n_rows;
+  // queries as the A operand, straight from memory; rows past the item's are zeros
+  uint32_t qa[D / 16][4];
+  int limit[2];                          // keys that the lane's rows see
 #pragma unroll
-  for (int m = 0; m < kM; ++m)
+  for (int hi = 0; hi < 2; ++hi) {
+    const int r = hi * 8 + quad;
+    const bool there = r < n_rows;
+    const int rr = there ? r : 0, tok = rr / p.G, h = k.head * p.G + rr - tok * p.G;
+    const uint32_t *src = reinterpret_cast<const uint32_t *>(p.q + ((size_t)(k.x.q_row0 + tok) * p.Hq + h) * D) + in_quad;
+    limit[hi] = own ? k.x.len - (k.x.rows - 1 - tok) : k.x.len;
 #pragma unroll
-    for (int hi = 0; hi < 2; ++hi) {
-      const int r = m * 16 + hi * 8 + quad;
-      const bool there = r < n_rows;
-      const int rr = k.row_tile * kRows + (there ? r : 0), tok = rr / p.G, h = k.head * p.G + rr - tok * p.G;
-      const uint32_t *src = reinterpret_cast<const uint32_t *>(p.q + ((size_t)(k.x.q_row0 + tok) * p.Hq + h) * D) + in_quad;
-      limit[m][hi] = own ? k.x.len - (k.x.rows - 1 - tok) : k.x.len;
-#pragma unroll
-      for (int c = 0; c < D / 16; ++c) {
-        qa[m][c][hi] = there ? __ldg(src + c * 8) : 0u;
-        qa[m][c][hi + 2] = there ? __ldg(src + c * 8 + 4) : 0u;
-      }
+    for (int c = 0; c < D / 16; ++c) {
+      qa[c][hi] = there ? __ldg(src + c * 8) : 0u;
+      qa[c][hi + 2] = there ? __ldg(src + c * 8 + 4) : 0u;
     }
-  float o[kM][D / 8][4], mx[kM][2], sum[kM][2];
-#pragma unroll
-  for (int m = 0; m < kM; ++m) {
-#pragma unroll
-    for (int c = 0; c < D / 8; ++c) o[m][c][0] = o[m][c][1] = o[m][c][2] = o[m][c][3] = 0.f;
-    mx[m][0] = mx[m][1] = -INFINITY; sum[m][0] = sum[m][1] = 0.f;
   }
+  float o[D / 8][4], mx[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f};
+#pragma unroll
+  for (int c = 0; c < D / 8; ++c) o[c][0] = o[c][1] = o[c][2] = o[c][3] = 0.f;
   const float sl = p.scale_log2;
   const int k_row = warp * 16 + ((lane >> 4) & 1) * 8 + (lane & 7), k_col = (lane >> 3) & 1;
   const int v_row = warp * 16 + ((lane >> 3) & 1) * 8 + (lane & 7), v_col = (lane >> 4) & 1;
@@ -203,66 +266,61 @@ __device__ __forceinline__ void consume_piece(const SharedParams &p, const Piece
     const int left = k.x.len - key0;
     const int ks = ring % L::kStages, vs = (ring + 1) % L::kStages;
     if (ok) ok = mbar_wait(&ctrl->full[ks], (ring / L::kStages) & 1, abort_flag);
-    float s[kM][2][4];
+    ok = __all_sync(0xffffffffu, ok);
+    float s[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
     if (ok && left > 0) {
       const uint32_t tile = smem_u32(smem + ks * L::kTileBytes) + k_row * 128;
-#pragma unroll
-      for (int m = 0; m < kM; ++m)
-#pragma unroll
-        for (int n = 0; n < 2; ++n) s[m][n][0] = s[m][n][1] = s[m][n][2] = s[m][n][3] = 0.f;
 #pragma unroll
       for (int c = 0; c < D / 16; ++c) {
         uint32_t b[4];
         const int col = c * 2 + k_col;
         ldsm4(b, tile + (col >> 3) * L::kRegion + (((col & 7) ^ (k_row & 7)) << 4));
-#pragma unroll
-        for (int m = 0; m < kM; ++m) { mma_16816(s[m][0], qa[m][c], b[0], b[1]); mma_16816(s[m][1], qa[m][c], b[2], b[3]); }
+        mma_16816(s[0], qa[c], b[0], b[1]);
+        mma_16816(s[1], qa[c], b[2], b[3]);
       }
     }
     __syncwarp();
     if (lane == 0) mbar_arrive(&ctrl->empty[ks]);
-    uint32_t pa[kM][4];
+    uint32_t pa[4];
     if (ok && left > 0) {
+      float top[2];
 #pragma unroll
-      for (int m = 0; m < kM; ++m) {
-        const bool masked = key0 + 16 > min(limit[m][0], limit[m][1]);
-        float top[2];
+      for (int hi = 0; hi < 2; ++hi) {
+        if (key0 + 16 > limit[hi]) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (key0 + (i >> 1) * 8 + in_quad * 2 + (i & 1) >= limit[hi]) s[i >> 1][hi * 2 + (i & 1)] = -INFINITY;
+        }
+        top[hi] = fmaxf(fmaxf(s[0][hi * 2], s[0][hi * 2 + 1]), fmaxf(s[1][hi * 2], s[1][hi * 2 + 1]));
+        top[hi] = fmaxf(top[hi], __shfl_xor_sync(0xffffffffu, top[hi], 1));
+        top[hi] = fmaxf(top[hi], __shfl_xor_sync(0xffffffffu, top[hi], 2));
+        top[hi] = fmaxf(top[hi], mx[hi]);
+      }
+      // (from -inf: yes, unless nothing has been seen yet)
+      const bool grow = (top[0] > mx[0] && !((top[0] - mx[0]) * sl <= kRescale)) || (top[1] > mx[1] && !((top[1] - mx[1]) * sl <= kRescale));
+      if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll
         for (int hi = 0; hi < 2; ++hi) {
-          if (masked) {
+          const float alpha = mx[hi] == -INFINITY ? 0.f : ex2((mx[hi] - top[hi]) * sl);     // (nothing summed so far)
+          mx[hi] = top[hi];
+          sum[hi] *= alpha;
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              if (key0 + (i >> 1) * 8 + in_quad * 2 + (i & 1) >= limit[m][hi]) s[m][i >> 1][hi * 2 + (i & 1)] = -INFINITY;
-          }
-          top[hi] = fmaxf(fmaxf(s[m][0][hi * 2], s[m][0][hi * 2 + 1]), fmaxf(s[m][1][hi * 2], s[m][1][hi * 2 + 1]));
-          top[hi] = fmaxf(top[hi], __shfl_xor_sync(0xffffffffu, top[hi], 1));
-          top[hi] = fmaxf(top[hi], __shfl_xor_sync(0xffffffffu, top[hi], 2));
-          top[hi] = fmaxf(top[hi], mx[m][hi]);
+          for (int c = 0; c < D / 8; ++c) { o[c][hi * 2] *= alpha; o[c][hi * 2 + 1] *= alpha; }
         }
-        const bool grow = (top[0] > mx[m][0] && !((top[0] - mx[m][0]) * sl <= kRescale)) || (top[1] > mx[m][1] && !((top[1] - mx[m][1]) * sl <= kRescale));
-        if (__any_sync(0xffffffffu, grow)) {
+      }
 #pragma unroll
-          for (int hi = 0; hi < 2; ++hi) {
-            const float alpha = mx[m][hi] == -INFINITY ? 0.f : ex2((mx[m][hi] - top[hi]) * sl);     // (nothing summed so far)
-            mx[m][hi] = top[hi];
-            sum[m][hi] *= alpha;
+      for (int hi = 0; hi < 2; ++hi) {
+        const float neg = mx[hi] == -INFINITY ? 0.f : -mx[hi] * sl;
+        float e[4];
 #pragma unroll
-            for (int c = 0; c < D / 8; ++c) { o[m][c][hi * 2] *= alpha; o[m][c][hi * 2 + 1] *= alpha; }
-          }
-        }
-#pragma unroll
-        for (int hi = 0; hi < 2; ++hi) {
-          const float neg = mx[m][hi] == -INFINITY ? 0.f : -mx[m][hi] * sl;
-          float e[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) e[i] = ex2(fmaf(s[m][i >> 1][hi * 2 + (i & 1)], sl, neg));
-          sum[m][hi] += (e[0] + e[1]) + (e[2] + e[3]);
-          pa[m][hi] = pack_bf16(e[0], e[1]);
-          pa[m][hi + 2] = pack_bf16(e[2], e[3]);
-        }
+        for (int i = 0; i < 4; ++i) e[i] = ex2(fmaf(s[i >> 1][hi * 2 + (i & 1)], sl, neg));
+        sum[hi] += (e[0] + e[1]) + (e[2] + e[3]);
+        pa[hi] = pack_bf16(e[0], e[1]);
+        pa[hi + 2] = pack_bf16(e[2], e[3]);
       }
     }
     if (ok) ok = mbar_wait(&ctrl->full[vs], ((ring + 1) / L::kStages) & 1, abort_flag);
+    ok = __all_sync(0xffffffffu, ok);
     if (ok && left > 0) {
       uint8_t *tile = smem + vs * L::kTileBytes;
       if (left < 16) {
@@ -280,8 +338,8 @@ __device__ __forceinline__ void consume_piece(const SharedParams &p, const Piece
         uint32_t b[4];
         const int col = c * 2 + v_col;
         ldsm4_t(b, base + (col >> 3) * L::kRegion + (((col & 7) ^ (v_row & 7)) << 4));
-#pragma unroll
-        for (int m = 0; m < kM; ++m) { mma_16816(o[m][2 * c], pa[m], b[0], b[1]); mma_16816(o[m][2 * c + 1], pa[m], b[2], b[3]); }
+        mma_16816(o[2 * c], pa, b[0], b[1]);
+        mma_16816(o[2 * c + 1], pa, b[2], b[3]);
       }
     }
     __syncwarp();
@@ -292,69 +350,414 @@ __device__ __forceinline__ void consume_piece(const SharedParams &p, const Piece
   float2 *stat = reinterpret_cast<float2 *>(smem + L::kStat);
   float *buf = reinterpret_cast<float *>(smem + L::kBuf);
 #pragma unroll
-  for (int m = 0; m < kM; ++m)
-#pragma unroll
-    for (int hi = 0; hi < 2; ++hi) {
-      sum[m][hi] += __shfl_xor_sync(0xffffffffu, sum[m][hi], 1);
-      sum[m][hi] += __shfl_xor_sync(0xffffffffu, sum[m][hi], 2);
-      if (in_quad == 0) stat[warp * kRows + m * 16 + hi * 8 + quad] = make_float2(mx[m][hi], sum[m][hi]);
-    }
+  for (int hi = 0; hi < 2; ++hi) {
+    sum[hi] += __shfl_xor_sync(0xffffffffu, sum[hi], 1);
+    sum[hi] += __shfl_xor_sync(0xffffffffu, sum[hi], 2);
+    if (in_quad == 0) stat[warp * kRows + hi * 8 + quad] = make_float2(mx[hi], sum[hi]);
+  }
   consumers_sync();
-  float *slot = p.part + (size_t)k.slot * L::kSlot;
-  const bool fits = k.slot < p.n_slots;                    // (always, by the host's count; a table that changes meanwhile would not)
+  // a row's place: in the output, among the first pieces, or in the CTA's own
+  auto place = [&](int r) -> long long {
+    return direct ? first_part(p, k.x, r, k.head, 0) : k.tile0 == 0 ? first_part(p, k.x, r, k.head, own ? 0 : 1) : cut_part(p, (int)blockIdx.x) + r;
+  };
+  float f[2];
 #pragma unroll
-  for (int m = 0; m < kM; ++m) {
-    float f[2];
+  for (int hi = 0; hi < 2; ++hi) {
+    const int r = hi * 8 + quad;
+    float top = -INFINITY, den = 0.f;
 #pragma unroll
-    for (int hi = 0; hi < 2; ++hi) {
-      const int r = m * 16 + hi * 8 + quad;
-      float top = -INFINITY, den = 0.f;
+    for (int w = 0; w < kWarps; ++w) top = fmaxf(top, stat[w * kRows + r].x);
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) top = fmaxf(top, stat[w * kRows + r].x);
+    for (int w = 0; w < kWarps; ++w) {
+      const float2 v = stat[w * kRows + r];
+      if (v.x != -INFINITY) den += v.y * ex2((v.x - top) * sl);
+    }
+    f[hi] = mx[hi] != -INFINITY && den > 0.f ? ex2((mx[hi] - top) * sl) / den : 0.f;
+    if (ok && warp == 0 && in_quad == 0 && r < n_rows) {
+      const float lse = den > 0.f ? (top * sl + log2f(den)) * 0.6931471805599453f : -INFINITY;
+      if (!direct) p.part[p.n_part * D + place(r)] = lse;
+      else if (p.lse) p.lse[place(r)] = lse;
+    }
+  }
+#pragma unroll
+  for (int half = 0; half < D / 64; ++half) {
+    float *mine = buf + warp * 16 * L::kBufStride;
+#pragma unroll
+    for (int c = 0; c < 8; ++c)
+#pragma unroll
+      for (int hi = 0; hi < 2; ++hi)
+        *reinterpret_cast<float2 *>(mine + (hi * 8 + quad) * L::kBufStride + c * 8 + in_quad * 2) =
+            make_float2(o[half * 8 + c][hi * 2] * f[hi], o[half * 8 + c][hi * 2 + 1] * f[hi]);
+    consumers_sync();
+    const int r = threadIdx.x >> 4, col = (threadIdx.x & 15) * 4;
+    if (ok && r < n_rows) {
+      float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (int w = 0; w < kWarps; ++w) {
-        const float2 v = stat[w * kRows + r];
-        if (v.x != -INFINITY) den += v.y * ex2((v.x - top) * sl);
+        const float4 v = *reinterpret_cast<const float4 *>(buf + (w * 16 + r) * L::kBufStride + col);
+        t.x += v.x; t.y += v.y; t.z += v.z; t.w += v.w;
       }
-      f[hi] = mx[m][hi] != -INFINITY && den > 0.f ? ex2((mx[m][hi] - top) * sl) / den : 0.f;
-      if (ok && warp == 0 && in_quad == 0 && r < n_rows) {
-        const float lse = den > 0.f ? (top * sl + log2f(den)) * 0.6931471805599453f : -INFINITY;
-        if (!direct) {
-          if (fits) slot[kRows * D + r] = lse;
-        } else if (p.lse) {
-          const int rr = k.row_tile * kRows + r, tok = rr / p.G;
-          p.lse[(size_t)(k.x.q_row0 + tok) * p.Hq + k.head * p.G + rr - tok * p.G] = lse;
+      const long long at = place(r) * D + half * 64 + col;
+      if (!direct) *reinterpret_cast<float4 *>(p.part + at) = t;
+      else if (p.out_f32) *reinterpret_cast<float4 *>(reinterpret_cast<float *>(p.o) + at) = t;
+      else *reinterpret_cast<uint2 *>(reinterpret_cast<__nv_bfloat16 *>(p.o) + at) = make_uint2(pack_bf16(t.x, t.y), pack_bf16(t.z, t.w));
+    }
+    consumers_sync();
+  }
+}
+
+// A CTA for few rows: units [begin, end) of that stream.
+template <int D>
+__device__ __forceinline__ void few_rows(const SharedParams &p, const CUtensorMap *tmap_kx, const CUtensorMap *tmap_vx, const CUtensorMap *tmap_k,
+                                         const CUtensorMap *tmap_v, uint8_t *smem, SharedCtrl *ctrl, const int *units, int n_entries, int begin, int end) {
+  using L = SharedLayout<D>;
+  const int warp = threadIdx.x >> 5;
+  int ring = 0;
+  bool ok = true;
+  if (warp >= kWarps) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kCopyRegs));
+    if (warp == kWarps) {
+      for (int at = begin; at < end && ok;) {
+        const Piece k = piece_at(p, units, n_entries, at, end);
+        at += k.n;
+        const bool own = k.e >= p.n_groups;
+        const Source src = source_of(p, k);
+        int next = box_row(p, src, k.tile0);               // (looked up a tile ahead)
+        for (int j = 0; j < k.n && ok; ++j) {
+          const int row = next;
+          if (j + 1 < k.n) next = box_row(p, src, k.tile0 + j + 1);
+          for (int kv = 0; kv < 2; ++kv, ++ring) {
+            const int stage = ring % L::kStages;
+            ok = mbar_wait(&ctrl->empty[stage], ((ring / L::kStages) & 1) ^ 1, &ctrl->abort_flag);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            copy_tile<D>(src, own ? (kv ? tmap_v : tmap_k) : (kv ? tmap_vx : tmap_kx), smem + stage * L::kTileBytes, &ctrl->full[stage], k.head, row);
+          }
         }
+      }
+      if (!ok) {
+        // leave no copy in flight: wait (bounded) for the tiles already requested
+        for (int i = max(0, ring - L::kStages); i < ring; ++i)
+          for (uint32_t spin = 0; spin < (1u << 20); ++spin)
+            if (mbar_try_wait(&ctrl->full[i % L::kStages], (i / L::kStages) & 1)) break;
       }
     }
-#pragma unroll
-    for (int half = 0; half < D / 64; ++half) {
-      float *mine = buf + warp * 16 * L::kBufStride;
-#pragma unroll
-      for (int c = 0; c < 8; ++c)
-#pragma unroll
-        for (int hi = 0; hi < 2; ++hi)
-          *reinterpret_cast<float2 *>(mine + (hi * 8 + quad) * L::kBufStride + c * 8 + in_quad * 2) =
-              make_float2(o[m][half * 8 + c][hi * 2] * f[hi], o[m][half * 8 + c][hi * 2 + 1] * f[hi]);
-      consumers_sync();
-      const int r = threadIdx.x >> 4, col = (threadIdx.x & 15) * 4;
-      if (ok && m * 16 + r < n_rows) {
-        float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
-          const float4 v = *reinterpret_cast<const float4 *>(buf + (w * 16 + r) * L::kBufStride + col);
-          t.x += v.x; t.y += v.y; t.z += v.z; t.w += v.w;
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kConsumerRegs));
+    for (int at = begin; at < end;) {                      // (to the end even after a wait that expired: the warps meet at barriers)
+      const Piece k = piece_at(p, units, n_entries, at, end);
+      at += k.n;
+      bool direct = k.e >= p.n_groups && k.n == k.tiles;
+      if (direct) {
+        const int g = group_of(p, k.e - p.n_groups);
+        direct = g < 0 || __ldg(p.prefix_cu + g + 1) == __ldg(p.prefix_cu + g);
+      }
+      consume_piece<D>(p, k, smem, ctrl, ring, ok, direct);
+    }
+  }
+}
+
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+__device__ __forceinline__ void copy_16_or_zero(uint32_t dst, const void *src, bool there) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+
+// A CTA for many rows: units [begin, end) of that stream.  Softmax group t has, of the n key tiles of a piece, all (a piece of more
+// than 128 rows: pair) or t, t + 2, ..
+template <int D>
+__device__ __forceinline__ void many_rows(const SharedParams &p, const CUtensorMap *tmap_kx, const CUtensorMap *tmap_vx, const CUtensorMap *tmap_k,
+                                          const CUtensorMap *tmap_v, uint8_t *smem, SharedCtrl *ctrl, const int *units, int n_entries, int begin, int end) {
+  using L = SharedLayout<D>;
+  constexpr int kDepth = L::kDepth;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t tmem = ctrl->tmem_base;
+  volatile int *abort_flag = &ctrl->abort_flag;
+  uint64_t *k_full = ctrl->full, *v_full = ctrl->full + 4, *k_empty = ctrl->empty, *v_empty = ctrl->empty + 4;
+  bool ok = true;
+  if (warp == 8) {
+    // ------------------------------------------------------------ copies: K_0, K_1, V_0, K_2, V_1, ..
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kServiceRegs));
+    int nk = 0, nv = 0;                                    // tiles of keys and of values requested so far
+    for (int at = begin; at < end && ok;) {
+      const Piece k = piece_at(p, units, n_entries, at, end);
+      at += k.n;
+      const bool own = k.e >= p.n_groups;
+      const Source src = source_of(p, k);
+      int next = box_row(p, src, k.tile0), before = -1;
+      for (int j = 0; j <= k.n && ok; ++j) {
+        const int row = next;
+        if (j + 1 < k.n) next = box_row(p, src, k.tile0 + j + 1);
+        if (j < k.n) {
+          const int st = nk % kDepth;
+          ok = __all_sync(0xffffffffu, mbar_wait(&k_empty[st], ((nk / kDepth) & 1) ^ 1, abort_flag));
+          if (!ok) break;
+          copy_tile<D>(src, own ? tmap_k : tmap_kx, smem + L::kKeys + st * L::kTileBytes, &k_full[st], k.head, row);
+          ++nk;
         }
-        if (!direct) {
-          if (fits) *reinterpret_cast<float4 *>(slot + (m * 16 + r) * D + half * 64 + col) = t;
+        if (j > 0) {
+          const int st = nv % kDepth;
+          ok = __all_sync(0xffffffffu, mbar_wait(&v_empty[st], ((nv / kDepth) & 1) ^ 1, abort_flag));
+          if (!ok) break;
+          copy_tile<D>(src, own ? tmap_v : tmap_vx, smem + L::kValues + st * L::kTileBytes, &v_full[st], k.head, before);
+          ++nv;
+        }
+        before = row;
+      }
+    }
+    if (!ok) {
+      // leave no copy in flight: wait (bounded) for the tiles already requested
+      for (int i = max(0, nk - kDepth); i < nk; ++i)
+        for (uint32_t spin = 0; spin < (1u << 20); ++spin)
+          if (mbar_try_wait(&k_full[i % kDepth], (i / kDepth) & 1)) break;
+      for (int i = max(0, nv - kDepth); i < nv; ++i)
+        for (uint32_t spin = 0; spin < (1u << 20); ++spin)
+          if (mbar_try_wait(&v_full[i % kDepth], (i / kDepth) & 1)) break;
+    }
+  } else if (warp == 9) {
+    // ------------------------------------------------------------ products
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kServiceRegs));
+    if (elect_one()) {
+      constexpr uint32_t idesc_qk = make_idesc_bf16(128, kTile, 0), idesc_pv = make_idesc_bf16(128, D, 1);
+      const uint64_t q_desc = make_smem_desc(smem_u32(smem), 16, 1024);
+      const uint64_t k_desc = make_smem_desc(smem_u32(smem + L::kKeys), 16, 1024);
+      const uint64_t v_desc = make_smem_desc(smem_u32(smem + L::kValues), L::kRegion, 1024);
+      int nk = 0, nv = 0, n_pieces = 0;                    // tiles of all earlier pieces; pieces
+      int p_uses[2] = {0, 0}, o_uses[2] = {0, 0};
+      for (int at = begin; at < end && ok;) {
+        const Piece k = piece_at(p, units, n_entries, at, end);
+        at += k.n;
+        const bool pair = k.n_rows > 128;
+        const int n = k.n, step = pair ? 1 : 2;
+        auto wait_k = [&](int j) { return mbar_wait(&k_full[(nk + j) % kDepth], ((nk + j) / kDepth) & 1, abort_flag); };
+        auto wait_v = [&](int j) { return mbar_wait(&v_full[(nv + j) % kDepth], ((nv + j) / kDepth) & 1, abort_flag); };
+        auto issue_qk = [&](int t, int j) {
+          const uint64_t qd = q_desc + (uint64_t)((pair && t ? L::kTileBytes : 0) >> 4);
+          const uint64_t kd = k_desc + (uint64_t)((((nk + j) % kDepth) * L::kTileBytes) >> 4);
+#pragma unroll
+          for (int c = 0; c < D / 16; ++c) {
+            const uint64_t off = (uint64_t)(((c >> 2) * L::kRegion + (c & 3) * 32) >> 4);
+            mma_ss(tmem + t * 128, qd + off, kd + off, idesc_qk, c > 0);
+          }
+          mma_commit(&ctrl->s_full[t]);
+          if (!pair || t) mma_commit(&k_empty[(nk + j) % kDepth]);
+          if (j + 1 == n && (!pair || t)) mma_commit(&ctrl->q_empty);         // that was the piece's last product with the queries
+        };
+        auto issue_pv = [&](int t, int j, bool first, int half) {
+          const uint64_t vd = v_desc + (uint64_t)((((nv + j) % kDepth) * L::kTileBytes) >> 4);
+#pragma unroll
+          for (int c = half * 4; c < half * 4 + 4; ++c)
+            mma_ts(tmem + 256 + t * 128, tmem + t * 128 + c * 8, vd + (uint64_t)((c * 2048) >> 4), idesc_pv, (!first || c > 0) ? 1u : 0u);
+        };
+        ok = mbar_wait(&ctrl->q_full, n_pieces & 1, abort_flag);
+        ++n_pieces;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const int j = pair ? 0 : t;
+          if (!ok || j >= n) continue;
+          ok = wait_k(j);
+          if (!ok) continue;
+          tc_fence_after();
+          issue_qk(t, j);
+        }
+        for (int i = 0; ok && i * step < n; ++i) {
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            const int j = pair ? i : 2 * i + t, jn = j + step;
+            if (!ok || j >= n) continue;
+            const bool last = jn >= n;
+            ok = wait_v(j);
+            // the first product of a piece overwrites O_t: the rows before it must have been read out
+            if (ok && i == 0) ok = mbar_wait(&ctrl->o_free[t], (o_uses[t] & 1) ^ 1, abort_flag);
+            if (ok) ok = mbar_wait(&ctrl->p_full[t][0], p_uses[t] & 1, abort_flag);
+            if (!ok) continue;
+            tc_fence_after();
+            issue_pv(t, j, i == 0, 0);
+            if (!last) ok = wait_k(jn);                    // (needed right after; off the critical path here)
+            if (ok) ok = mbar_wait(&ctrl->p_full[t][1], p_uses[t] & 1, abort_flag);
+            if (!ok) continue;
+            tc_fence_after();
+            issue_pv(t, j, false, 1);
+            ++p_uses[t];
+            if (last) { mma_commit(&ctrl->o_done[t]); ++o_uses[t]; }
+            if (!pair || t) mma_commit(&v_empty[(nv + j) % kDepth]);
+            if (!last) issue_qk(t, jn);
+          }
+        }
+        nk += n; nv += n;
+      }
+    }
+  } else if (warp >= 10) {
+    // ------------------------------------------------------------ queries: 16 bytes a copy, into the tiles' swizzled layout
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kServiceRegs));
+    int n_pieces = 0;
+    for (int at = begin; at < end && ok; ++n_pieces) {
+      const Piece k = piece_at(p, units, n_entries, at, end);
+      at += k.n;
+      ok = mbar_wait(&ctrl->q_empty, (n_pieces & 1) ^ 1, abort_flag);
+      if (!ok) break;
+      constexpr int kVecs = D / 8;
+      const int tile_rows = k.n_rows > 128 ? 256 : 128;
+      const uint32_t base = smem_u32(smem);
+      for (int i = threadIdx.x - 320; i < tile_rows * kVecs; i += 64) {
+        const int r = i / kVecs, c = i % kVecs;
+        const bool there = r < k.n_rows;                   // (rows that are not there are zeros: they take part in no maximum)
+        const int rr = k.row0 + (there ? r : 0), tok = rr / p.G;
+        const __nv_bfloat16 *src = p.q + ((size_t)(k.x.q_row0 + tok) * p.Hq + k.head * p.G + rr - tok * p.G) * D + c * 8;
+        copy_16_or_zero(base + (r >> 7) * L::kTileBytes + (c >> 3) * L::kRegion + (r & 127) * 128 + (((c & 7) ^ (r & 7)) << 4), src, there);
+      }
+      asm volatile("cp.async.wait_all;" ::: "memory");
+      fence_proxy_async();                                 // the tensor core reads through the async proxy
+      mbar_arrive(&ctrl->q_full);
+    }
+  } else {
+    // ------------------------------------------------------------ softmax, a thread a row
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
+    const int t = warp >> 2, r = threadIdx.x & 127;
+    const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
+    const uint32_t tS = tmem + t * 128 + lane_off, tO = tmem + 256 + t * 128 + lane_off;
+    const float sl = p.scale_log2;
+    int s_uses = 0, o_uses = 0, nv = 0;
+    for (int at = begin; at < end && ok;) {
+      const Piece k = piece_at(p, units, n_entries, at, end);
+      at += k.n;
+      const bool pair = k.n_rows > 128, own = k.e >= p.n_groups;
+      const int step = pair ? 1 : 2, row = pair ? t * 128 + r : r;             // of the item
+      const int limit = own ? k.x.len - (k.x.rows - 1 - min(k.x.rows - 1, (k.row0 + row) / p.G)) : k.x.len;
+      float m_used = -INFINITY, l = 0.f;
+      const int j0 = pair ? 0 : t;
+      for (int j = j0; j < k.n; j += step) {
+        ok = __all_sync(0xffffffffu, mbar_wait(&ctrl->s_full[t], s_uses & 1, abort_flag));
+        if (!ok) break;
+        ++s_uses;
+        tc_fence_after();
+        const int key0 = (k.tile0 + j) * kTile, lim = limit - key0;            // columns 0 .. lim - 1 are seen
+        uint32_t s[128];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) tmem_ld_32x32b_x32(tS + c * 32, *reinterpret_cast<uint32_t(*)[32]>(&s[c * 32]));
+        tmem_wait_ld();
+        if (lim < 128) {
+#pragma unroll
+          for (int c = 0; c < 128; ++c)
+            if (c >= lim) s[c] = 0xff800000u;                                  // -inf
+        }
+        const float *sf = reinterpret_cast<const float *>(s);
+        float l1[43], l2[15], l3[5];
+#pragma unroll
+        for (int i = 0; i < 43; ++i) l1[i] = 3 * i + 2 < 128 ? max3(sf[3 * i], sf[3 * i + 1], sf[3 * i + 2]) : fmaxf(sf[126], sf[127]);
+#pragma unroll
+        for (int i = 0; i < 15; ++i) l2[i] = 3 * i + 2 < 43 ? max3(l1[3 * i], l1[3 * i + 1], l1[3 * i + 2]) : l1[42];
+#pragma unroll
+        for (int i = 0; i < 5; ++i) l3[i] = max3(l2[3 * i], l2[3 * i + 1], l2[3 * i + 2]);
+        const float m_new = fmaxf(m_used, fmaxf(max3(l3[0], l3[1], l3[2]), fmaxf(l3[3], l3[4])));
+        if (j == j0) {
+          m_used = m_new;
         } else {
-          const int rr = k.row_tile * kRows + m * 16 + r, tok = rr / p.G;
-          const size_t at = ((size_t)(k.x.q_row0 + tok) * p.Hq + k.head * p.G + rr - tok * p.G) * D + half * 64 + col;
-          if (p.out_f32) *reinterpret_cast<float4 *>(reinterpret_cast<float *>(p.o) + at) = t;
-          else *reinterpret_cast<uint2 *>(reinterpret_cast<__nv_bfloat16 *>(p.o) + at) = make_uint2(pack_bf16(t.x, t.y), pack_bf16(t.z, t.w));
+          const bool grow = (m_new - m_used) * sl > kRescale;                  // (from -inf: yes)
+          if (__any_sync(0xffffffffu, grow)) {
+            // 1 when this row's maximum did not move (also when the row has seen no key yet)
+            const float alpha = (m_new == -INFINITY) ? 1.f : ex2((m_used - m_new) * sl);
+            m_used = m_new;
+            l *= alpha;
+#pragma unroll 1
+            for (int c = 0; c < D / 32; ++c) {
+              uint32_t o[32];
+              tmem_ld_32x32b_x32(tO + c * 32, o);
+              tmem_wait_ld();
+#pragma unroll
+              for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
+              tmem_st_32x32b_x32(tO + c * 32, o);
+            }
+          }
+        }
+        const float neg_m = (m_used == -INFINITY) ? 0.f : -m_used * sl;        // no key seen so far: every p is 0
+        const uint64_t sl2 = pack2(sl, sl), negm2 = pack2(neg_m, neg_m);
+        uint64_t sum2[4] = {0ull, 0ull, 0ull, 0ull};
+        // P is handed over in two halves, so that the product starts on the first 64 keys while the others are exponentiated
+        uint32_t pk[32], pk1[32];
+        auto expo = [&](int e0, uint32_t &dst, int i) {
+          const uint64_t x2 = fma2(pack2(__uint_as_float(s[e0]), __uint_as_float(s[e0 + 1])), sl2, negm2);
+          float x0, x1;
+          unpack2(x2, x0, x1);
+          const float p0 = ex2(x0), p1 = ex2(x1);
+          sum2[i & 3] = add2(sum2[i & 3], pack2(p0, p1));
+          dst = pack_bf16(p0, p1);
+        };
+#pragma unroll
+        for (int i = 0; i < 32; ++i) expo(2 * i, pk[i], i);
+        tmem_st_32x32b_x32(tS, pk);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) expo(64 + 2 * i, pk1[i], i);
+        const int valid = k.x.len - key0;
+        if (valid < kTile) {
+          // values behind the end may be anything, and zero times a NaN is a NaN: zeros there, before the product may start
+          const int jv = nv + j;
+          ok = __all_sync(0xffffffffu, mbar_wait(&v_full[jv % kDepth], (jv / kDepth) & 1, abort_flag));
+          if (!ok) break;
+          uint8_t *tile = smem + L::kValues + (jv % kDepth) * L::kTileBytes;
+          for (int i = r; i < (kTile - valid) * (D / 8); i += 128) {
+            const int vr = valid + i / (D / 8), c = i % (D / 8);
+            *reinterpret_cast<uint4 *>(tile + (c >> 3) * L::kRegion + vr * 128 + ((c & 7) << 4)) = make_uint4(0, 0, 0, 0);
+          }
+          fence_proxy_async();
+        }
+        tmem_wait_st();
+        tc_fence_before();
+        mbar_arrive(&ctrl->p_full[t][0]);
+#pragma unroll
+        for (int i = 16; i < 32; ++i) expo(64 + 2 * i, pk1[i], i);
+        tmem_st_32x32b_x32(tS + 32, pk1);
+        tmem_wait_st();
+        tc_fence_before();
+        mbar_arrive(&ctrl->p_full[t][1]);
+        float sum[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) unpack2(sum2[i], sum[2 * i], sum[2 * i + 1]);
+        l += ((sum[0] + sum[1]) + (sum[2] + sum[3])) + ((sum[4] + sum[5]) + (sum[6] + sum[7]));
+      }
+      nv += k.n;
+      if (!ok) break;
+      // The rows leave through shared memory, 16 columns at a time, so that a store writes 64 bytes of each of eight rows.
+      const int which = (own ? 0 : 1) + (pair ? 0 : 2 * t);
+      const int cut_row = pair ? 0 : t * 128;
+      auto place = [&](int rr) { return k.tile0 == 0 ? first_part(p, k.x, k.row0 + rr, k.head, which) : cut_part(p, (int)blockIdx.x) + cut_row + rr; };
+      const float lse = l > 0.f ? (m_used * sl + log2f(l)) * 0.6931471805599453f : -INFINITY;
+      if (row < k.n_rows) p.part[p.n_part * D + place(row)] = lse;
+      if (j0 >= k.n) continue;                             // (no tile for this group)
+      const float inv = l > 0.f ? 1.f / l : 0.f;
+      ok = __all_sync(0xffffffffu, mbar_wait(&ctrl->o_done[t], o_uses & 1, abort_flag));
+      ++o_uses;
+      if (!ok) break;
+      tc_fence_after();
+      float *stage = reinterpret_cast<float *>(smem + L::kOut) + warp * 32 * 16;
+      const int first = row - lane;                        // the warp's first row
+#pragma unroll 1
+      for (int c = 0; c < D / 32; ++c) {
+        uint32_t o[32];
+        tmem_ld_32x32b_x32(tO + c * 32, o);
+        tmem_wait_ld();
+        if (c + 1 == D / 32) { tc_fence_before(); mbar_arrive(&ctrl->o_free[t]); }     // O_t has been read out
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+#pragma unroll
+          for (int v = 0; v < 4; ++v)
+            *reinterpret_cast<float4 *>(stage + lane * 16 + ((v ^ ((lane >> 1) & 3)) << 2)) =
+                make_float4(__uint_as_float(o[half * 16 + v * 4]) * inv, __uint_as_float(o[half * 16 + v * 4 + 1]) * inv,
+                            __uint_as_float(o[half * 16 + v * 4 + 2]) * inv, __uint_as_float(o[half * 16 + v * 4 + 3]) * inv);
+          __syncwarp();
+#pragma unroll
+          for (int it = 0; it < 4; ++it) {
+            const int rr = it * 8 + (lane >> 2), v = lane & 3;
+            if (first + rr < k.n_rows)
+              *reinterpret_cast<float4 *>(p.part + place(first + rr) * D + c * 32 + half * 16 + v * 4) =
+                  *reinterpret_cast<const float4 *>(stage + rr * 16 + ((v ^ ((rr >> 1) & 3)) << 2));
+          }
+          __syncwarp();
         }
       }
-      consumers_sync();
     }
   }
 }
@@ -368,141 +771,102 @@ ba_shared_attend_kernel(const __grid_constant__ CUtensorMap tmap_kx, const __gri
   extern __shared__ uint8_t smem_raw[];
   uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   SharedCtrl *ctrl = reinterpret_cast<SharedCtrl *>(smem + L::kCtrl);
-  int *units = reinterpret_cast<int *>(smem + L::kUnits), *items = reinterpret_cast<int *>(smem + L::kItems);
+  int *units = reinterpret_cast<int *>(smem + L::kUnits);  // of entries of few rows; those of many behind them
+  int *units_many = units + kMaxEntries + 4;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int n_entries = p.n_groups + p.batch;
-  if (tid == 0) {
-    for (int s = 0; s < L::kStages; ++s) { mbar_init(&ctrl->full[s], 1); mbar_init(&ctrl->empty[s], kWarps); }
-    ctrl->abort_flag = 0; ctrl->invalid = 0;
-    fence_barrier_init();
-  }
+  const int n_entries = p.n_groups + p.batch, n_ctas = (int)gridDim.x;
+  if (tid == 0) { ctrl->abort_flag = 0; ctrl->invalid = 0; }
   if (warp == kWarps && elect_one()) { prefetch_tmap(&tmap_k); prefetch_tmap(&tmap_v); prefetch_tmap(&tmap_kx); prefetch_tmap(&tmap_vx); }
   ba_pdl_wait();
-  ba_pdl_trigger();
   __syncthreads();
-  // The stream: units (key tiles) and items of every entry, summed up.  A thread takes neighbouring entries.
-  {
-    const int per = (n_entries + kThreads - 1) / kThreads, e0 = min(n_entries, tid * per), e1 = min(n_entries, e0 + per);
-    bool good = true;
-    for (int e = e0; e < e1; ++e) good = good && entry_holds(p, e);
-    if (!good) ctrl->invalid = 1;
-    __syncthreads();
-    long long nu = 0, ni = 0;
-    if (!ctrl->invalid) {                                  // (groups read the queries' table of other threads' sequences)
-      for (int e = e0; e < e1; ++e) {
-        const Entry x = get_entry(p, e);
-        const long long it = (long long)row_tiles_of(p, x) * p.Hkv;
-        nu += it * tiles_of(x); ni += it;
+  // The streams: units (key tiles) before every entry, by kind, and what the entries of many rows cost.  A thread takes neighbouring entries.
+  const int per = (n_entries + kThreads - 1) / kThreads, e0 = min(n_entries, tid * per), e1 = min(n_entries, e0 + per);
+  bool good = true;
+  for (int e = e0; e < e1; ++e) good = good && entry_holds(p, e);
+  if (!good) ctrl->invalid = 1;
+  __syncthreads();
+  // (sums in doubles, whole numbers up to 2^53, so that what is too much shows)
+  double sum[2] = {0, 0}, cost = 0;
+  if (!ctrl->invalid) {                                    // (groups read the queries' table of other threads' sequences)
+    for (int e = e0; e < e1; ++e) {
+      const Entry x = get_entry(p, e);
+      const double items = (double)row_tiles_of(p, x) * p.Hkv, n = items * tiles_of(x);
+      sum[is_many(p, x)] += n;
+      if (is_many(p, x)) {
+        const int left = x.rows * p.G % kManyRows;         // (rows of the last item, if it is not full)
+        cost += n * kCostPair - (left > 0 && left <= 128 ? (double)p.Hkv * tiles_of(x) * (kCostPair - kCostSolo) : 0.);
       }
-      if (nu > INT32_MAX || ni > INT32_MAX) { nu = ni = 0; ctrl->invalid = 1; }
     }
-    // sums over the warp, then over the warps, in doubles: whole numbers up to 2^53, so that an overflow shows
-    double su = (double)nu, si = (double)ni;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      const double a = __shfl_up_sync(0xffffffffu, su, d), b = __shfl_up_sync(0xffffffffu, si, d);
-      if (lane >= d) { su += a; si += b; }
-    }
-    if (su > 2e9 || si > 2e9) ctrl->invalid = 1;
-    if (lane == 31) { ctrl->warp_units[warp] = su > 2e9 ? 0 : (int)su; ctrl->warp_items[warp] = si > 2e9 ? 0 : (int)si; }
-    __syncthreads();
-    for (int w = 0; w < warp; ++w) { su += ctrl->warp_units[w]; si += ctrl->warp_items[w]; }
-    if (su > 2e9 || si > 2e9) ctrl->invalid = 1;
-    __syncthreads();
-    if (!ctrl->invalid) {
-      int u = (int)(su - (double)nu), i = (int)(si - (double)ni);
-      for (int e = e0; e < e1; ++e) {
-        units[e] = u; items[e] = i;
-        const Entry x = get_entry(p, e);
-        const int it = row_tiles_of(p, x) * p.Hkv, tiles = tiles_of(x);
-        if (blockIdx.x == 0) p.meta[e] = make_int4(u, tiles, row_tiles_of(p, x), i);
-        u += it * tiles; i += it;
-      }
-      if (tid == kThreads - 1) { units[n_entries] = (int)su; items[n_entries] = (int)si; }
-    }
-    __syncthreads();
   }
-  const bool valid = !ctrl->invalid;
-  const int total = valid ? units[n_entries] : 0;
-  const int run = (total + (int)gridDim.x - 1) / (int)gridDim.x;
+  const double mine[2] = {sum[0], sum[1]};
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const double a = __shfl_up_sync(0xffffffffu, sum[0], d), b = __shfl_up_sync(0xffffffffu, sum[1], d), c = __shfl_up_sync(0xffffffffu, cost, d);
+    if (lane >= d) { sum[0] += a; sum[1] += b; cost += c; }
+  }
+  if (lane == 31) {
+    ctrl->warp_units[0][warp] = sum[0]; ctrl->warp_units[1][warp] = sum[1]; ctrl->warp_cost[warp] = cost;
+  }
+  __syncthreads();
+  double total[2] = {0, 0}, cost_many = 0;
+  for (int w = 0; w < kThreads / 32; ++w) {
+    if (w == warp) { sum[0] += total[0]; sum[1] += total[1]; }
+    total[0] += ctrl->warp_units[0][w]; total[1] += ctrl->warp_units[1][w]; cost_many += ctrl->warp_cost[w];
+  }
+  const bool valid = !ctrl->invalid && total[0] < 2e9 && total[1] < 2e9;
+  // CTAs for many rows
+  int n_many = 0;
+  if (total[1] > 0) {
+    n_many = (int)((double)n_ctas * cost_many / (cost_many + total[0] * kCostFew) + 0.5);
+    n_many = max(1, min(n_many, total[0] > 0 ? n_ctas - 1 : n_ctas));
+  }
+  const int n_few = n_ctas - n_many;
+  const int run[2] = {valid && n_few ? ((int)total[0] + n_few - 1) / n_few : 0, valid && n_many ? ((int)total[1] + n_many - 1) / n_many : 0};
+  if (valid) {
+    int u[2] = {(int)(sum[0] - mine[0]), (int)(sum[1] - mine[1])};
+    for (int e = e0; e < e1; ++e) {
+      units[e] = u[0]; units_many[e] = u[1];
+      const Entry x = get_entry(p, e);
+      const bool many = is_many(p, x);
+      if (blockIdx.x == 0) p.meta[e] = make_int4(u[many], tiles_of(x), x.rows * p.G, many);
+      u[many] += row_tiles_of(p, x) * p.Hkv * tiles_of(x);
+    }
+    if (tid == kThreads - 1) { units[n_entries] = (int)total[0]; units_many[n_entries] = (int)total[1]; }
+  }
   if (blockIdx.x == 0 && tid == 0) {
-    p.meta[n_entries] = make_int4(run, valid, 0, 0);
+    p.meta[n_entries] = make_int4(run[0], run[1], n_many, valid);
     if (!valid) ba_record_status(p.status, BA_ERR_INVALID_ARG);
   }
-  const int begin = (int)min((long long)total, (long long)run * blockIdx.x), end = min(total, begin + run);
-  if (begin < end) {
-    int ring = 0;
-    bool ok = true;
-    if (warp >= kWarps) {
-      asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kCopyRegs));
-      if (warp == kWarps) {
-        // ------------------------------------------------------------ copies
-        for (int at = begin; at < end && ok;) {
-          const Piece k = piece_at(p, units, items, n_entries, at, end);
-          at += k.n;
-          const bool own = k.e >= p.n_groups, paged = own || p.prefix_paged;
-          const CUtensorMap *mk = own ? &tmap_k : &tmap_kx, *mv = own ? &tmap_v : &tmap_vx;
-          const int lg = own ? p.page_lg : p.prefix_page_lg, n_pages = own ? p.n_pages : p.prefix_pages;
-          const int sub_rows = paged ? min(kTile, 1 << lg) : kTile;
-          const int list = own ? __ldg(p.page_cu + k.e - p.n_groups) : paged ? __ldg(p.prefix_page_cu + k.e) : 0;
-          const int32_t *idx = own ? p.page_idx : p.prefix_page_idx;
-          const int first = paged ? 0 : __ldg(p.prefix_cu + k.e);
-          // lane i has box i of a tile, a box per page; the row of its next box is looked up a tile ahead
-          auto row_of = [&](int tile) -> int {
-            const int t = tile * kTile + lane * sub_rows;
-            if (lane * sub_rows >= kTile || t >= k.x.len) return -1;
-            if (!paged) return first + t;
-            const int page = __ldg(idx + list + (t >> lg));
-            if (page < 0 || page >= n_pages) {
-              ba_record_status(p.status, BA_ERR_INVALID_ARG);
-              return n_pages << lg;                          // behind the pool: the copy engine fills in zeros
-            }
-            return (page << lg) + (t & ((1 << lg) - 1));
-          };
-          int next = row_of(k.tile0);
-          for (int j = 0; j < k.n && ok; ++j) {
-            const int row = next;
-            if (j + 1 < k.n) next = row_of(k.tile0 + j + 1);
-            const unsigned boxes = __popc(__ballot_sync(0xffffffffu, row >= 0));
-            for (int kv = 0; kv < 2; ++kv, ++ring) {
-              const int stage = ring % L::kStages;
-              ok = mbar_wait(&ctrl->empty[stage], ((ring / L::kStages) & 1) ^ 1, &ctrl->abort_flag);
-              ok = __all_sync(0xffffffffu, ok);
-              if (!ok) break;
-              if (lane == 0) mbar_arrive_expect_tx(&ctrl->full[stage], boxes * sub_rows * D * 2);
-              __syncwarp();
-              if (row >= 0) {
-                uint8_t *dst = smem + stage * L::kTileBytes + lane * sub_rows * 128;
-                for (int c = 0; c < L::kChunks; ++c) tma_load_3d(dst + c * L::kRegion, kv ? mv : mk, &ctrl->full[stage], c * 64, k.head, row);
-              }
-              __syncwarp();
-            }
-          }
-        }
-        if (!ok) {
-          // leave no copy in flight: wait (bounded) for the tiles already requested
-          for (int i = max(0, ring - L::kStages); i < ring; ++i)
-            for (uint32_t spin = 0; spin < (1u << 20); ++spin)
-              if (mbar_try_wait(&ctrl->full[i % L::kStages], (i / L::kStages) & 1)) break;
-        }
+  const bool many = (int)blockIdx.x < n_many;
+  const int nth = many ? (int)blockIdx.x : (int)blockIdx.x - n_many, all = valid ? (int)total[many] : 0;
+  const int begin = (int)min((long long)all, (long long)run[many] * nth), end = min(all, begin + run[many]);
+  if (tid == 0) {
+    if (many) {
+      for (int i = 0; i < 8; ++i) { mbar_init(&ctrl->full[i], 1); mbar_init(&ctrl->empty[i], 1); }
+      mbar_init(&ctrl->q_full, 64); mbar_init(&ctrl->q_empty, 1);
+      for (int t = 0; t < 2; ++t) {
+        mbar_init(&ctrl->s_full[t], 1); mbar_init(&ctrl->p_full[t][0], 128); mbar_init(&ctrl->p_full[t][1], 128);
+        mbar_init(&ctrl->o_done[t], 1); mbar_init(&ctrl->o_free[t], 128);
       }
     } else {
-      asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kConsumerRegs));
-      for (int at = begin; at < end;) {                    // (to the end even after a wait that expired: the warps meet at barriers)
-        const Piece k = piece_at(p, units, items, n_entries, at, end);
-        at += k.n;
-        bool direct = k.e >= p.n_groups && k.n == k.tiles;
-        if (direct) {
-          const int g = group_of(p, k.e - p.n_groups);
-          direct = g < 0 || units[g + 1] == units[g];
-        }
-        if (min(kRows, k.x.rows * p.G - k.row_tile * kRows) <= 16) consume_piece<D, 1>(p, k, smem, ctrl, ring, ok, direct);
-        else consume_piece<D, 2>(p, k, smem, ctrl, ring, ok, direct);
-      }
+      for (int i = 0; i < L::kStages; ++i) { mbar_init(&ctrl->full[i], 1); mbar_init(&ctrl->empty[i], kWarps); }
     }
+    fence_barrier_init();
   }
+  const bool tensor = many && begin < end;
+  if (tensor && warp == 9) { tmem_alloc(&ctrl->tmem_base, 512); tmem_relinquish(); }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  ba_pdl_trigger();
+  if (begin < end) {
+    if (many) many_rows<D>(p, &tmap_kx, &tmap_vx, &tmap_k, &tmap_v, smem, ctrl, units_many, n_entries, begin, end);
+    else few_rows<D>(p, &tmap_kx, &tmap_vx, &tmap_k, &tmap_v, smem, ctrl, units, n_entries, begin, end);
+  }
+  tc_fence_before();
   __syncthreads();
   if (tid == 0 && ctrl->abort_flag) ba_record_status(p.status, BA_ERR_TIMEOUT);
+  if (tensor && warp == 9) tmem_dealloc(ctrl->tmem_base, 512);
 }
 
 // The partial results of every (row, head): those of its group's prefix and of its own rows, weighted by their denominators.  A warp
@@ -510,13 +874,11 @@ ba_shared_attend_kernel(const __grid_constant__ CUtensorMap tmap_kx, const __gri
 template <int D>
 __global__ void __launch_bounds__(256)
 ba_shared_merge_kernel(const __grid_constant__ SharedParams p) {
-  using L = SharedLayout<D>;
   constexpr int kLanes = D / 4, kAt = 256 / kLanes;
   ba_pdl_wait();
   ba_pdl_trigger();
   const int4 head = p.meta[p.n_groups + p.batch];          // (plain loads: the kernel before wrote them)
-  if (!head.y) return;
-  const int run = head.x;
+  if (!head.w) return;
   const long long u = (long long)blockIdx.x * kAt + threadIdx.x / kLanes;
   const int c = threadIdx.x % kLanes;
   if (u >= (long long)p.n_q_rows * p.Hq) return;
@@ -531,7 +893,16 @@ ba_shared_merge_kernel(const __grid_constant__ SharedParams p) {
   const int g = group_of(p, s);
   float top = -INFINITY, den = 0.f;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  int pieces = 0;
+  auto add = [&](long long at) {
+    const float lse = p.part[p.n_part * D + at];
+    if (lse == -INFINITY) return;                          // no key seen: there are no values either
+    const float4 x = __ldcs(reinterpret_cast<const float4 *>(p.part + at * D) + c);
+    const float t = fmaxf(top, lse), fa = top == -INFINITY ? 0.f : __expf(top - t), fx = __expf(lse - t);
+    top = t;
+    den = den * fa + fx;
+    acc.x = acc.x * fa + x.x * fx; acc.y = acc.y * fa + x.y * fx; acc.z = acc.z * fa + x.z * fx; acc.w = acc.w * fa + x.w * fx;
+  };
+  bool beside = false;
 #pragma unroll 1
   for (int side = 0; side < 2; ++side) {
     const int e = side == 0 ? g : p.n_groups + s;
@@ -539,20 +910,19 @@ ba_shared_merge_kernel(const __grid_constant__ SharedParams p) {
     const int4 m = p.meta[e];
     if (m.y == 0) continue;
     const int row0 = side == 0 ? q_begin(p, p.group_cu ? __ldg(p.group_cu + g) : 0) : q_begin(p, s);
-    const int r = (row - row0) * p.G + hq - h * p.G, rt = r / kRows, item = h * m.z + rt;
-    const int a = m.x + item * m.y, c0 = a / run, c1 = (a + m.y - 1) / run;
-    if (side == 1 && pieces == 0 && c0 == c1) return;      // whole, and nothing beside it: written where it was computed
-    for (int k = c0; k <= c1; ++k, ++pieces) {
-      const int at = m.w + item + k;
-      if (at >= p.n_slots) return;
-      const float *slot = p.part + (size_t)at * L::kSlot;
-      const float lse = slot[kRows * D + r - rt * kRows];
-      if (lse == -INFINITY) continue;
-      const float4 x = __ldcs(reinterpret_cast<const float4 *>(slot + (r - rt * kRows) * D) + c);
-      const float t = fmaxf(top, lse), fa = top == -INFINITY ? 0.f : __expf(top - t), fx = __expf(lse - t);
-      top = t;
-      den = den * fa + fx;
-      acc.x = acc.x * fa + x.x * fx; acc.y = acc.y * fa + x.y * fx; acc.z = acc.z * fa + x.z * fx; acc.w = acc.w * fa + x.w * fx;
+    const int r = (row - row0) * p.G + hq - h * p.G, which = side == 0 ? 1 : 0;
+    const int rts = m.w ? (m.z + kManyRows - 1) / kManyRows : 1, rt = m.w ? r / kManyRows : 0, run = m.w ? head.y : head.x;
+    const bool two = m.w && m.z - rt * kManyRows <= 128;   // each softmax group left a result
+    const int a = m.x + (h * rts + rt) * m.y, c0 = a / run, c1 = (a + m.y - 1) / run, cta0 = m.w ? 0 : head.z;
+    if (side == 1 && !beside && c0 == c1 && !m.w) return;  // whole, and nothing beside it: written where it was computed
+    beside = true;
+    const long long here = (long long)row * p.Hq + hq, of_all = (long long)p.n_q_rows * p.Hq;
+    add(which * of_all + here);
+    if (two) add((which + 2) * of_all + here);
+    for (int k = c0 + 1; k <= c1; ++k) {
+      const long long at = cut_part(p, cta0 + k) + r - rt * kManyRows;
+      add(at);
+      if (two) add(at + 128);
     }
   }
   const float inv = den > 0.f ? 1.f / den : 0.f;
@@ -564,12 +934,8 @@ ba_shared_merge_kernel(const __grid_constant__ SharedParams p) {
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
-// Slots: a piece per item, and one more for every cut (one per CTA at most).  Items: row tiles of prefixes and of own rows, each
-// entry with one that is not full.
-long long slots_for(const ba_config &c, int batch, int n_groups, int n_q_rows, int n_ctas) {
-  const long long G = c.n_q_heads / c.n_kv_heads, rows = (long long)n_q_rows * G;
-  return (2 * (rows / kRows) + n_groups + batch) * c.n_kv_heads + n_ctas;
-}
+// Rows of partial results: four for every (query row, head), and kManyRows a CTA.
+long long part_rows(const ba_config &c, int n_q_rows, int n_ctas) { return 4ll * n_q_rows * c.n_q_heads + (long long)n_ctas * kManyRows; }
 size_t meta_bytes(int n_entries) { return ba_align_up((size_t)(n_entries + 1) * sizeof(int4), 256); }
 constexpr int kMostCtas = 256;        // sizing without a device
 
@@ -590,7 +956,7 @@ ba_status ba_shared_prefix_bytes(const ba_config *cfg, int32_t batch, int32_t n_
   if (!bytes || batch < 1 || n_groups < 0 || n_q_rows < 0) return BA_ERR_INVALID_ARG;
   if ((long long)batch + n_groups > BA_SHARED_MAX) return BA_ERR_UNSUPPORTED;
   *bytes = ba_scratch_offset(nullptr) + meta_bytes(batch + n_groups) +
-           (size_t)slots_for(*cfg, batch, n_groups, n_q_rows, kMostCtas) * kRows * (cfg->head_dim + 1) * sizeof(float) + 256;
+           (size_t)part_rows(*cfg, n_q_rows, kMostCtas) * (cfg->head_dim + 1) * sizeof(float) + 256;
   return BA_OK;
 }
 
@@ -614,10 +980,10 @@ ba_status ba_shared_prefix_attend(ba_ctx *ctx, const void *q, int32_t n_q_rows, 
   }
   if (b->batch == 0 || n_q_rows == 0) return BA_OK;
   const int D = ctx->cfg.head_dim, n_entries = b->batch + b->n_groups;
-  const long long n_slots = slots_for(ctx->cfg, b->batch, b->n_groups, n_q_rows, ctx->sm_count);
-  const size_t need = meta_bytes(n_entries) + (size_t)n_slots * kRows * (D + 1) * sizeof(float);
+  const long long n_part = part_rows(ctx->cfg, n_q_rows, ctx->sm_count);
+  const size_t need = meta_bytes(n_entries) + (size_t)n_part * (D + 1) * sizeof(float);
   if (!ctx->workspace || ba_scratch_offset(ctx) + need + ctx->pending_table_bytes > ctx->workspace_bytes) return BA_ERR_WORKSPACE;
-  if (n_slots > INT32_MAX || (long long)n_q_rows * ctx->cfg.n_q_heads > INT32_MAX) return BA_ERR_SHAPE;
+  if ((long long)n_q_rows * ctx->cfg.n_q_heads > INT32_MAX) return BA_ERR_SHAPE;
   BA_CUDA_TRY(cudaSetDevice(ctx->device));
   auto lg_of = [](const ba_page_table *t) { int lg = 0; while ((1 << lg) < t->page_rows) ++lg; return lg; };
   SharedParams p = {};
@@ -638,7 +1004,7 @@ ba_status ba_shared_prefix_attend(ba_ctx *ctx, const void *q, int32_t n_q_rows, 
   char *scratch = (char *)ctx->workspace + ba_scratch_offset(ctx);
   p.meta = (int4 *)scratch;
   p.part = (float *)(scratch + meta_bytes(n_entries));
-  p.n_slots = (int)n_slots;
+  p.n_part = n_part;
   CUtensorMap tk, tv, tkx, tvx;
   const long long rows = (long long)pages->n_pages * pages->page_rows;
   const int box = std::min(kTile, pages->page_rows);

@@ -337,6 +337,10 @@ CASES = {
     "rows before their keys, prefix": ([20], [0, 3], [9, 5, 2], [4, 0, 300], 16, False),
     "no queries": ([90], [0, 4], [0, 2, 0, 3], [10, 11, 0, 300], 256, False),
     "long": ([5000], [0, 3], [1, 2, 1], [2500, 1, 700], 16, True),
+    "many rows": ([3000, 130], [0, 5, 9], [20, 1, 40, 3, 60, 1, 1, 1, 1], [20, 5, 300, 3, 700, 0, 1, 128, 200], 32, False),
+    "items cut often": ([9000], [0, 3], [70, 1, 2], [100, 30, 2], 16, True),
+    "many rows of their own": ([], [0], [50, 40], [1000, 2000], 64, True),
+    "both kinds": ([40, 2000, 3], [0, 1, 2, 40], [3, 30] + [1] * 38, [100] * 40, 128, False),
     "many": ([64, 200], [0, 70, 150], [1] * 150, [i % 140 for i in range(150)], 16, False),
 }
 
