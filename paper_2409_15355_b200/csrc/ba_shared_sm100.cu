@@ -4,7 +4,8 @@
 // are (token, head of a KV group) pairs; its keys come in tiles of 128.  Entries are of two kinds, by their rows:
 //   few  (at most 16): a key is used by few rows, the bytes of the cache are all that counts.  An item is entry x KV head.
 //   many (more): a matrix product.  An item is entry x KV head x 256 rows (two tiles of 128), for the tensor core.
-// The key tiles of all items of a kind, laid end to end, are a stream that is cut into equal runs, one per CTA; the CTAs are shared out
+// The key tiles of all items of a kind, laid end to end (an item begins with a few units that stand for what it costs besides them), are
+// a stream that is cut into equal runs, one per CTA; the CTAs are shared out
 // among the two streams by their cost.  So one long sequence, many short ones and a prefix of 32K keep every SM equally long.
 // An item that a cut divides leaves partial results (normalised rows and their log-sum-exp), in the rows of its queries for its first
 // piece and in a place of the CTA for the others (a run starts with one such piece at most); a second kernel merges them, prefix
@@ -42,6 +43,8 @@ constexpr int kConsumerRegs = 224, kCopyRegs = 56;
 constexpr int kMaxEntries = BA_SHARED_MAX;
 constexpr int kSoftmaxRegs = 208, kServiceRegs = 88;     // of CTAs for many rows: 256 * 208 + 128 * 88
 // What a key tile costs, to share out the CTAs: two query tiles, one, and few rows (cycles / 1000).
+// Units that an item counts for besides its key tiles: what begins and ends it (queries, the pipeline's filling, the rows' way out).
+constexpr int kItemMany = 3, kItemFew = 1;
 constexpr double kCostPair = 4., kCostSolo = 3., kCostFew = 3.;
 constexpr float kRescale = 8.f;       // O is rescaled when a maximum grows by more than 2^8: exact in real arithmetic, values stay bounded
 
@@ -65,6 +68,8 @@ struct SharedParams {
   int4 *meta;                         // [n_groups + batch]: first unit in its stream, tiles, rows, many; then runs of the two kinds, CTAs for many, validity
 };
 
+constexpr int kCtrlBytes = 1088;
+
 template <int D>
 struct SharedLayout {
   static constexpr int kTileBytes = kTile * D * 2;
@@ -83,18 +88,20 @@ struct SharedLayout {
   static constexpr int kEnd = kFewEnd > kManyEnd ? kFewEnd : kManyEnd;
   static constexpr int kUnits = (kEnd + 15) / 16 * 16;                 // [2][kMaxEntries + 4]: units before an entry, by kind
   static constexpr int kCtrl = kUnits + 2 * (kMaxEntries + 4) * 4;
-  static constexpr int kBytes = kCtrl + 640 + 1024;
+  static constexpr int kBytes = kCtrl + kCtrlBytes + 1024;
 };
 static_assert(SharedLayout<128>::kBytes <= 227 * 1024, "shared memory");
 
 struct SharedCtrl {
-  uint64_t full[10], empty[10];       // few: the ring; many: keys [0 .. 3], values [4 .. 7]
+  uint64_t full[10], empty[10];       // few: the ring
+  uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4];                       // many
   uint64_t q_full, q_empty, s_full[2], p_full[2][2], o_done[2], o_free[2];
   int abort_flag, invalid;
   uint32_t tmem_base;
+  uint32_t alone[kMaxEntries / 32];   // a bit an entry: own rows of a sequence without prefix
   double warp_units[2][kThreads / 32], warp_cost[kThreads / 32];
 };
-static_assert(sizeof(SharedCtrl) <= 640, "control area");
+static_assert(sizeof(SharedCtrl) <= kCtrlBytes, "control area");
 
 // An entry, looked up by the thread that asks: rows q_row0 .. of the queries, `len` keys.
 struct Entry { int q_row0, rows, len; };
@@ -112,31 +119,49 @@ __device__ __forceinline__ Entry get_entry(const SharedParams &p, int e) {
   }
   return x;
 }
-// The tables of entry e hold: nothing else of them is read where they do not.
-__device__ __forceinline__ bool entry_holds(const SharedParams &p, int e) {
+// The same with its tables checked: false, and nothing read by their values, where they do not hold.
+__device__ __forceinline__ bool load_entry(const SharedParams &p, int e, Entry &x) {
+  x.q_row0 = x.rows = x.len = 0;
+  int a, b;
   if (e < p.n_groups) {
-    if (p.group_cu) {
-      const int a = __ldg(p.group_cu + e), b = __ldg(p.group_cu + e + 1);
-      if (a < 0 || b < a || b > p.batch) return false;
-    }
+    a = p.group_cu ? __ldg(p.group_cu + e) : 0; b = p.group_cu ? __ldg(p.group_cu + e + 1) : p.batch;
     const int r0 = __ldg(p.prefix_cu + e), r1 = __ldg(p.prefix_cu + e + 1);
-    if (r0 < 0 || r1 < r0) return false;
-    if (!p.prefix_paged) return r1 <= p.n_prefix_rows;
-    return (long long)(r1 - r0) <= ((long long)__ldg(p.prefix_page_cu + e + 1) - __ldg(p.prefix_page_cu + e)) << p.prefix_page_lg;
+    const long long room = p.prefix_paged ? ((long long)__ldg(p.prefix_page_cu + e + 1) - __ldg(p.prefix_page_cu + e)) << p.prefix_page_lg : p.n_prefix_rows - r0;
+    if (a < 0 || b < a || b > p.batch || r0 < 0 || r1 < r0 || r1 - r0 > room) return false;
+    x.len = r1 - r0;
+  } else {
+    const int s = e - p.n_groups, len = __ldg(p.own_len + s);
+    const long long room = ((long long)__ldg(p.page_cu + s + 1) - __ldg(p.page_cu + s)) << p.page_lg;
+    if (len < 0 || len > room) return false;
+    a = s; b = s + 1; x.len = len;
   }
-  const int s = e - p.n_groups, a = q_begin(p, s), b = q_begin(p, s + 1), len = __ldg(p.own_len + s);
-  if (a < 0 || b < a || b > p.n_q_rows || len < 0) return false;
-  return len == 0 || (long long)len <= ((long long)__ldg(p.page_cu + s + 1) - __ldg(p.page_cu + s)) << p.page_lg;
+  x.q_row0 = q_begin(p, a); x.rows = q_begin(p, b) - x.q_row0;
+  return x.q_row0 >= 0 && x.rows >= 0 && x.q_row0 + x.rows <= p.n_q_rows;
 }
 __device__ __forceinline__ int tiles_of(const Entry &x) { return (x.len + kTile - 1) / kTile; }
 __device__ __forceinline__ bool is_many(const SharedParams &p, const Entry &x) { return x.rows * p.G > kRows; }
 __device__ __forceinline__ int row_tiles_of(const SharedParams &p, const Entry &x) { return is_many(p, x) ? (x.rows * p.G + kManyRows - 1) / kManyRows : x.rows > 0; }
-// Index in the partial results of row r of an entry, head h, of an item's first piece: `which` 0 own rows, 1 a prefix, + 2 the second
-// softmax group's.
-__device__ __forceinline__ long long first_part(const SharedParams &p, const Entry &x, int r, int h, int which) {
-  const int tok = r / p.G;
-  return ((long long)which * p.n_q_rows + x.q_row0 + tok) * p.Hq + h * p.G + r - tok * p.G;
+__device__ __forceinline__ int item_units(const SharedParams &p, const Entry &x) {
+  const int tiles = tiles_of(x);
+  return tiles > 0 ? tiles + (is_many(p, x) ? kItemMany : kItemFew) : 0;
 }
+// Rows of an item: row r is head h of token tok of its queries (tok x heads + h) from `at` on.
+struct RowMap {
+  long long at;         // of its first token and head, as o is indexed without the head's values
+  int g0, G, Hq;
+  float inv;
+  __device__ __forceinline__ RowMap(const SharedParams &p, const Entry &x, int row0, int head) : G(p.G), Hq(p.Hq), inv(1.f / (float)p.G) {
+    const int tok0 = row0 / p.G;
+    g0 = row0 - tok0 * p.G;
+    at = (long long)(x.q_row0 + tok0) * p.Hq + head * p.G;
+  }
+  // tokens from the first one to row r's (whole numbers below G + 256: exact)
+  __device__ __forceinline__ int token(int r) const { return (int)(((float)(g0 + r) + 0.5f) * inv); }
+  __device__ __forceinline__ long long row(int r) const { const int t = token(r); return at + (long long)t * Hq + (g0 + r - t * G); }
+};
+// First pieces leave their results at the rows of their queries: `which` 0 own rows, 1 a prefix, + 2 the second softmax group's; other pieces
+// at their CTA's.
+__device__ __forceinline__ long long first_part(const SharedParams &p, int which) { return (long long)which * p.n_q_rows * p.Hq; }
 __device__ __forceinline__ long long cut_part(const SharedParams &p, int cta) { return 4ll * p.n_q_rows * p.Hq + (long long)cta * kManyRows; }
 
 // Last index in x[0 .. n] whose value is at most v (x[0] = 0 <= v).
@@ -156,20 +181,23 @@ __device__ __forceinline__ int group_of(const SharedParams &p, int s) {
 
 // A piece of a stream: key tiles tile0 .. tile0 + n - 1 of an item, rows row0 .. row0 + n_rows - 1 of its entry.
 struct Piece {
-  int e, head, row0, n_rows, tile0, n, tiles;
+  int e, head, row0, n_rows, tile0, n, tiles, units;
   Entry x;
 };
-// The piece that starts at unit `at` of this CTA's run, which ends at `end`.
+// The piece that starts at unit `at` of this CTA's run, which ends at `end`; units is where it stops.  n = 0: only units in front of the tiles.
 __device__ __forceinline__ Piece piece_at(const SharedParams &p, const int *units, int n_entries, int at, int end) {
   Piece k;
   k.e = last_at_most(units, n_entries, at);
   k.x = get_entry(p, k.e);
   k.tiles = tiles_of(k.x);
-  const int local = at - units[k.e], item = local / k.tiles, rts = row_tiles_of(p, k.x);
-  k.tile0 = local - item * k.tiles;
+  const int item_all = item_units(p, k.x), front = item_all - k.tiles, begin = units[k.e];
+  const int item = (at - begin) / item_all, rts = row_tiles_of(p, k.x), from = at - begin - item * item_all;
   k.head = item / rts; k.row0 = (item - k.head * rts) * kManyRows;
   k.n_rows = min(kManyRows, k.x.rows * p.G - k.row0);
-  k.n = min(k.tiles - k.tile0, end - at);
+  const int to = min(item_all, from + end - at);
+  k.units = to - from;
+  k.tile0 = max(0, from - front);
+  k.n = max(0, to - front) - k.tile0;
   return k;
 }
 // Where the keys of a piece lie.  Lane i of the copying warp has box i of a tile, a box per page.
@@ -239,6 +267,7 @@ __device__ __forceinline__ void consume_piece(const SharedParams &p, const Piece
   volatile int *abort_flag = &ctrl->abort_flag;
   const bool own = k.e >= p.n_groups;
   const int n_rows = k.n_rows;
+  const RowMap map(p, k.x, 0, k.head);
   // queries as the A operand, straight from memory; rows past the item's are zeros
   uint32_t qa[D / 16][4];
   int limit[2];                          // keys that the lane's rows see
@@ -246,9 +275,8 @@ __device__ __forceinline__ void consume_piece(const SharedParams &p, const Piece
   for (int hi = 0; hi < 2; ++hi) {
     const int r = hi * 8 + quad;
     const bool there = r < n_rows;
-    const int rr = there ? r : 0, tok = rr / p.G, h = k.head * p.G + rr - tok * p.G;
-    const uint32_t *src = reinterpret_cast<const uint32_t *>(p.q + ((size_t)(k.x.q_row0 + tok) * p.Hq + h) * D) + in_quad;
-    limit[hi] = own ? k.x.len - (k.x.rows - 1 - tok) : k.x.len;
+    const uint32_t *src = reinterpret_cast<const uint32_t *>(p.q + map.row(there ? r : 0) * D) + in_quad;
+    limit[hi] = own ? k.x.len - (k.x.rows - 1 - map.token(there ? r : 0)) : k.x.len;
 #pragma unroll
     for (int c = 0; c < D / 16; ++c) {
       qa[c][hi] = there ? __ldg(src + c * 8) : 0u;
@@ -358,7 +386,7 @@ __device__ __forceinline__ void consume_piece(const SharedParams &p, const Piece
   consumers_sync();
   // a row's place: in the output, among the first pieces, or in the CTA's own
   auto place = [&](int r) -> long long {
-    return direct ? first_part(p, k.x, r, k.head, 0) : k.tile0 == 0 ? first_part(p, k.x, r, k.head, own ? 0 : 1) : cut_part(p, (int)blockIdx.x) + r;
+    return direct ? map.row(r) : k.tile0 == 0 ? first_part(p, own ? 0 : 1) + map.row(r) : cut_part(p, (int)blockIdx.x) + r;
   };
   float f[2];
 #pragma unroll
@@ -419,7 +447,8 @@ __device__ __forceinline__ void few_rows(const SharedParams &p, const CUtensorMa
     if (warp == kWarps) {
       for (int at = begin; at < end && ok;) {
         const Piece k = piece_at(p, units, n_entries, at, end);
-        at += k.n;
+        at += k.units;
+        if (k.n == 0) continue;
         const bool own = k.e >= p.n_groups;
         const Source src = source_of(p, k);
         int next = box_row(p, src, k.tile0);               // (looked up a tile ahead)
@@ -446,12 +475,9 @@ __device__ __forceinline__ void few_rows(const SharedParams &p, const CUtensorMa
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kConsumerRegs));
     for (int at = begin; at < end;) {                      // (to the end even after a wait that expired: the warps meet at barriers)
       const Piece k = piece_at(p, units, n_entries, at, end);
-      at += k.n;
-      bool direct = k.e >= p.n_groups && k.n == k.tiles;
-      if (direct) {
-        const int g = group_of(p, k.e - p.n_groups);
-        direct = g < 0 || __ldg(p.prefix_cu + g + 1) == __ldg(p.prefix_cu + g);
-      }
+      at += k.units;
+      if (k.n == 0) continue;
+      const bool direct = k.e >= p.n_groups && k.n == k.tiles && (ctrl->alone[k.e >> 5] >> (k.e & 31) & 1);
       consume_piece<D>(p, k, smem, ctrl, ring, ok, direct);
     }
   }
@@ -476,7 +502,7 @@ __device__ __forceinline__ void many_rows(const SharedParams &p, const CUtensorM
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t tmem = ctrl->tmem_base;
   volatile int *abort_flag = &ctrl->abort_flag;
-  uint64_t *k_full = ctrl->full, *v_full = ctrl->full + 4, *k_empty = ctrl->empty, *v_empty = ctrl->empty + 4;
+  uint64_t *k_full = ctrl->k_full, *v_full = ctrl->v_full, *k_empty = ctrl->k_empty, *v_empty = ctrl->v_empty;
   bool ok = true;
   if (warp == 8) {
     // ------------------------------------------------------------ copies: K_0, K_1, V_0, K_2, V_1, ..
@@ -484,7 +510,8 @@ __device__ __forceinline__ void many_rows(const SharedParams &p, const CUtensorM
     int nk = 0, nv = 0;                                    // tiles of keys and of values requested so far
     for (int at = begin; at < end && ok;) {
       const Piece k = piece_at(p, units, n_entries, at, end);
-      at += k.n;
+      at += k.units;
+      if (k.n == 0) continue;
       const bool own = k.e >= p.n_groups;
       const Source src = source_of(p, k);
       int next = box_row(p, src, k.tile0), before = -1;
@@ -529,7 +556,8 @@ __device__ __forceinline__ void many_rows(const SharedParams &p, const CUtensorM
       int p_uses[2] = {0, 0}, o_uses[2] = {0, 0};
       for (int at = begin; at < end && ok;) {
         const Piece k = piece_at(p, units, n_entries, at, end);
-        at += k.n;
+        at += k.units;
+        if (k.n == 0) continue;
         const bool pair = k.n_rows > 128;
         const int n = k.n, step = pair ? 1 : 2;
         auto wait_k = [&](int j) { return mbar_wait(&k_full[(nk + j) % kDepth], ((nk + j) / kDepth) & 1, abort_flag); };
@@ -594,20 +622,21 @@ __device__ __forceinline__ void many_rows(const SharedParams &p, const CUtensorM
     // ------------------------------------------------------------ queries: 16 bytes a copy, into the tiles' swizzled layout
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kServiceRegs));
     int n_pieces = 0;
-    for (int at = begin; at < end && ok; ++n_pieces) {
+    for (int at = begin; at < end && ok;) {
       const Piece k = piece_at(p, units, n_entries, at, end);
-      at += k.n;
+      at += k.units;
+      if (k.n == 0) continue;
       ok = mbar_wait(&ctrl->q_empty, (n_pieces & 1) ^ 1, abort_flag);
       if (!ok) break;
+      ++n_pieces;
       constexpr int kVecs = D / 8;
-      const int tile_rows = k.n_rows > 128 ? 256 : 128;
-      const uint32_t base = smem_u32(smem);
-      for (int i = threadIdx.x - 320; i < tile_rows * kVecs; i += 64) {
-        const int r = i / kVecs, c = i % kVecs;
+      const int tile_rows = k.n_rows > 128 ? 256 : 128, c = (threadIdx.x - 320) % kVecs;
+      const RowMap map(p, k.x, k.row0, k.head);
+      const uint32_t base = smem_u32(smem) + (c >> 3) * L::kRegion;
+#pragma unroll 8
+      for (int r = (threadIdx.x - 320) / kVecs; r < tile_rows; r += 64 / kVecs) {
         const bool there = r < k.n_rows;                   // (rows that are not there are zeros: they take part in no maximum)
-        const int rr = k.row0 + (there ? r : 0), tok = rr / p.G;
-        const __nv_bfloat16 *src = p.q + ((size_t)(k.x.q_row0 + tok) * p.Hq + k.head * p.G + rr - tok * p.G) * D + c * 8;
-        copy_16_or_zero(base + (r >> 7) * L::kTileBytes + (c >> 3) * L::kRegion + (r & 127) * 128 + (((c & 7) ^ (r & 7)) << 4), src, there);
+        copy_16_or_zero(base + (r >> 7) * L::kTileBytes + (r & 127) * 128 + (((c & 7) ^ (r & 7)) << 4), p.q + map.row(there ? r : 0) * D + c * 8, there);
       }
       asm volatile("cp.async.wait_all;" ::: "memory");
       fence_proxy_async();                                 // the tensor core reads through the async proxy
@@ -623,7 +652,8 @@ __device__ __forceinline__ void many_rows(const SharedParams &p, const CUtensorM
     int s_uses = 0, o_uses = 0, nv = 0;
     for (int at = begin; at < end && ok;) {
       const Piece k = piece_at(p, units, n_entries, at, end);
-      at += k.n;
+      at += k.units;
+      if (k.n == 0) continue;
       const bool pair = k.n_rows > 128, own = k.e >= p.n_groups;
       const int step = pair ? 1 : 2, row = pair ? t * 128 + r : r;             // of the item
       const int limit = own ? k.x.len - (k.x.rows - 1 - min(k.x.rows - 1, (k.row0 + row) / p.G)) : k.x.len;
@@ -721,9 +751,9 @@ __device__ __forceinline__ void many_rows(const SharedParams &p, const CUtensorM
       nv += k.n;
       if (!ok) break;
       // The rows leave through shared memory, 16 columns at a time, so that a store writes 64 bytes of each of eight rows.
-      const int which = (own ? 0 : 1) + (pair ? 0 : 2 * t);
-      const int cut_row = pair ? 0 : t * 128;
-      auto place = [&](int rr) { return k.tile0 == 0 ? first_part(p, k.x, k.row0 + rr, k.head, which) : cut_part(p, (int)blockIdx.x) + cut_row + rr; };
+      const RowMap map(p, k.x, k.row0, k.head);
+      const long long base = k.tile0 == 0 ? first_part(p, (own ? 0 : 1) + (pair ? 0 : 2 * t)) : cut_part(p, (int)blockIdx.x) + (pair ? 0 : t * 128);
+      auto place = [&](int rr) { return base + (k.tile0 == 0 ? map.row(rr) : rr); };
       const float lse = l > 0.f ? (m_used * sl + log2f(l)) * 0.6931471805599453f : -INFINITY;
       if (row < k.n_rows) p.part[p.n_part * D + place(row)] = lse;
       if (j0 >= k.n) continue;                             // (no tile for this group)
@@ -733,7 +763,12 @@ __device__ __forceinline__ void many_rows(const SharedParams &p, const CUtensorM
       if (!ok) break;
       tc_fence_after();
       float *stage = reinterpret_cast<float *>(smem + L::kOut) + warp * 32 * 16;
-      const int first = row - lane;                        // the warp's first row
+      float *dst[4];                                       // of the lane's rows of the warp's 32
+#pragma unroll
+      for (int it = 0; it < 4; ++it) {
+        const int rr = row - lane + it * 8 + (lane >> 2);
+        dst[it] = rr < k.n_rows ? p.part + place(rr) * D + (lane & 3) * 4 : nullptr;
+      }
 #pragma unroll 1
       for (int c = 0; c < D / 32; ++c) {
         uint32_t o[32];
@@ -751,9 +786,7 @@ __device__ __forceinline__ void many_rows(const SharedParams &p, const CUtensorM
 #pragma unroll
           for (int it = 0; it < 4; ++it) {
             const int rr = it * 8 + (lane >> 2), v = lane & 3;
-            if (first + rr < k.n_rows)
-              *reinterpret_cast<float4 *>(p.part + place(first + rr) * D + c * 32 + half * 16 + v * 4) =
-                  *reinterpret_cast<const float4 *>(stage + rr * 16 + ((v ^ ((rr >> 1) & 3)) << 2));
+            if (dst[it]) *reinterpret_cast<float4 *>(dst[it] + c * 32 + half * 16) = *reinterpret_cast<const float4 *>(stage + rr * 16 + ((v ^ ((rr >> 1) & 3)) << 2));
           }
           __syncwarp();
         }
@@ -775,29 +808,43 @@ ba_shared_attend_kernel(const __grid_constant__ CUtensorMap tmap_kx, const __gri
   int *units_many = units + kMaxEntries + 4;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int n_entries = p.n_groups + p.batch, n_ctas = (int)gridDim.x;
-  if (tid == 0) { ctrl->abort_flag = 0; ctrl->invalid = 0; }
+  if (tid == 0) {
+    for (int i = 0; i < L::kStages; ++i) { mbar_init(&ctrl->full[i], 1); mbar_init(&ctrl->empty[i], kWarps); }
+    for (int i = 0; i < L::kDepth; ++i) { mbar_init(&ctrl->k_full[i], 1); mbar_init(&ctrl->k_empty[i], 1); mbar_init(&ctrl->v_full[i], 1); mbar_init(&ctrl->v_empty[i], 1); }
+    mbar_init(&ctrl->q_full, 64); mbar_init(&ctrl->q_empty, 1);
+    for (int t = 0; t < 2; ++t) {
+      mbar_init(&ctrl->s_full[t], 1); mbar_init(&ctrl->p_full[t][0], 128); mbar_init(&ctrl->p_full[t][1], 128);
+      mbar_init(&ctrl->o_done[t], 1); mbar_init(&ctrl->o_free[t], 128);
+    }
+    ctrl->abort_flag = 0; ctrl->invalid = 0;
+    fence_barrier_init();
+  }
+  if (tid >= 32 && tid < 32 + kMaxEntries / 32) ctrl->alone[tid - 32] = 0;
+  if (warp == 9) { tmem_alloc(&ctrl->tmem_base, 512); tmem_relinquish(); }
   if (warp == kWarps && elect_one()) { prefetch_tmap(&tmap_k); prefetch_tmap(&tmap_v); prefetch_tmap(&tmap_kx); prefetch_tmap(&tmap_vx); }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
   ba_pdl_wait();
-  __syncthreads();
-  // The streams: units (key tiles) before every entry, by kind, and what the entries of many rows cost.  A thread takes neighbouring entries.
+  ba_pdl_trigger();
+  // The streams: units before every entry, by kind, and what the entries of many rows cost.  A thread takes neighbouring entries.
   const int per = (n_entries + kThreads - 1) / kThreads, e0 = min(n_entries, tid * per), e1 = min(n_entries, e0 + per);
-  bool good = true;
-  for (int e = e0; e < e1; ++e) good = good && entry_holds(p, e);
-  if (!good) ctrl->invalid = 1;
-  __syncthreads();
-  // (sums in doubles, whole numbers up to 2^53, so that what is too much shows)
   double sum[2] = {0, 0}, cost = 0;
-  if (!ctrl->invalid) {                                    // (groups read the queries' table of other threads' sequences)
-    for (int e = e0; e < e1; ++e) {
-      const Entry x = get_entry(p, e);
-      const double items = (double)row_tiles_of(p, x) * p.Hkv, n = items * tiles_of(x);
-      sum[is_many(p, x)] += n;
-      if (is_many(p, x)) {
-        const int left = x.rows * p.G % kManyRows;         // (rows of the last item, if it is not full)
-        cost += n * kCostPair - (left > 0 && left <= 128 ? (double)p.Hkv * tiles_of(x) * (kCostPair - kCostSolo) : 0.);
-      }
+  Entry one;                                               // (a thread's only entry, where there are no more than threads)
+  for (int e = e0; e < e1; ++e) {
+    if (!load_entry(p, e, one)) { ctrl->invalid = 1; one.len = one.rows = 0; }
+    const double n = (double)row_tiles_of(p, one) * p.Hkv * item_units(p, one);
+    sum[is_many(p, one)] += n;
+    if (is_many(p, one)) {
+      const int left = one.rows * p.G % kManyRows;         // (rows of the last item, if it is not full)
+      cost += n * kCostPair - (left > 0 && left <= 128 ? (double)p.Hkv * item_units(p, one) * (kCostPair - kCostSolo) : 0.);
+    }
+    if (e >= p.n_groups) {
+      const int g = group_of(p, e - p.n_groups);
+      if (g < 0 || __ldg(p.prefix_cu + g + 1) == __ldg(p.prefix_cu + g)) atomicOr(&ctrl->alone[e >> 5], 1u << (e & 31));
     }
   }
+  // (sums in doubles, whole numbers up to 2^53, so that what is too much shows)
   const double mine[2] = {sum[0], sum[1]};
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
@@ -826,10 +873,10 @@ ba_shared_attend_kernel(const __grid_constant__ CUtensorMap tmap_kx, const __gri
     int u[2] = {(int)(sum[0] - mine[0]), (int)(sum[1] - mine[1])};
     for (int e = e0; e < e1; ++e) {
       units[e] = u[0]; units_many[e] = u[1];
-      const Entry x = get_entry(p, e);
+      const Entry x = per == 1 ? one : get_entry(p, e);
       const bool many = is_many(p, x);
       if (blockIdx.x == 0) p.meta[e] = make_int4(u[many], tiles_of(x), x.rows * p.G, many);
-      u[many] += row_tiles_of(p, x) * p.Hkv * tiles_of(x);
+      u[many] += row_tiles_of(p, x) * p.Hkv * item_units(p, x);
     }
     if (tid == kThreads - 1) { units[n_entries] = (int)total[0]; units_many[n_entries] = (int)total[1]; }
   }
@@ -840,25 +887,7 @@ ba_shared_attend_kernel(const __grid_constant__ CUtensorMap tmap_kx, const __gri
   const bool many = (int)blockIdx.x < n_many;
   const int nth = many ? (int)blockIdx.x : (int)blockIdx.x - n_many, all = valid ? (int)total[many] : 0;
   const int begin = (int)min((long long)all, (long long)run[many] * nth), end = min(all, begin + run[many]);
-  if (tid == 0) {
-    if (many) {
-      for (int i = 0; i < 8; ++i) { mbar_init(&ctrl->full[i], 1); mbar_init(&ctrl->empty[i], 1); }
-      mbar_init(&ctrl->q_full, 64); mbar_init(&ctrl->q_empty, 1);
-      for (int t = 0; t < 2; ++t) {
-        mbar_init(&ctrl->s_full[t], 1); mbar_init(&ctrl->p_full[t][0], 128); mbar_init(&ctrl->p_full[t][1], 128);
-        mbar_init(&ctrl->o_done[t], 1); mbar_init(&ctrl->o_free[t], 128);
-      }
-    } else {
-      for (int i = 0; i < L::kStages; ++i) { mbar_init(&ctrl->full[i], 1); mbar_init(&ctrl->empty[i], kWarps); }
-    }
-    fence_barrier_init();
-  }
-  const bool tensor = many && begin < end;
-  if (tensor && warp == 9) { tmem_alloc(&ctrl->tmem_base, 512); tmem_relinquish(); }
-  tc_fence_before();
   __syncthreads();
-  tc_fence_after();
-  ba_pdl_trigger();
   if (begin < end) {
     if (many) many_rows<D>(p, &tmap_kx, &tmap_vx, &tmap_k, &tmap_v, smem, ctrl, units_many, n_entries, begin, end);
     else few_rows<D>(p, &tmap_kx, &tmap_vx, &tmap_k, &tmap_v, smem, ctrl, units, n_entries, begin, end);
@@ -866,22 +895,21 @@ ba_shared_attend_kernel(const __grid_constant__ CUtensorMap tmap_kx, const __gri
   tc_fence_before();
   __syncthreads();
   if (tid == 0 && ctrl->abort_flag) ba_record_status(p.status, BA_ERR_TIMEOUT);
-  if (tensor && warp == 9) tmem_dealloc(ctrl->tmem_base, 512);
+  if (warp == 9) tmem_dealloc(ctrl->tmem_base, 512);
 }
 
-// The partial results of every (row, head): those of its group's prefix and of its own rows, weighted by their denominators.  A warp
-// has a row of 128 values, or two of 64.
+// The partial results of every (row, head): those of its group's prefix and of its own rows, weighted by their denominators.  A warp has a
+// row of an output head; what it waits for is looked up side by side.
 template <int D>
 __global__ void __launch_bounds__(256)
 ba_shared_merge_kernel(const __grid_constant__ SharedParams p) {
-  constexpr int kLanes = D / 4, kAt = 256 / kLanes;
+  constexpr int kV = D / 32;                               // columns of a lane
+  const int lane = threadIdx.x & 31;
+  const long long u = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
   ba_pdl_wait();
   ba_pdl_trigger();
   const int4 head = p.meta[p.n_groups + p.batch];          // (plain loads: the kernel before wrote them)
-  if (!head.w) return;
-  const long long u = (long long)blockIdx.x * kAt + threadIdx.x / kLanes;
-  const int c = threadIdx.x % kLanes;
-  if (u >= (long long)p.n_q_rows * p.Hq) return;
+  if (!head.w || u >= (long long)p.n_q_rows * p.Hq) return;
   const int row = (int)(u / p.Hq), hq = (int)(u - (long long)row * p.Hq), h = hq / p.G;
   int s = row;
   if (p.q_cu) {
@@ -891,45 +919,81 @@ ba_shared_merge_kernel(const __grid_constant__ SharedParams p) {
   }
   if (s < 0 || s >= p.batch) return;
   const int g = group_of(p, s);
-  float top = -INFINITY, den = 0.f;
-  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  auto add = [&](long long at) {
-    const float lse = p.part[p.n_part * D + at];
-    if (lse == -INFINITY) return;                          // no key seen: there are no values either
-    const float4 x = __ldcs(reinterpret_cast<const float4 *>(p.part + at * D) + c);
-    const float t = fmaxf(top, lse), fa = top == -INFINITY ? 0.f : __expf(top - t), fx = __expf(lse - t);
-    top = t;
-    den = den * fa + fx;
-    acc.x = acc.x * fa + x.x * fx; acc.y = acc.y * fa + x.y * fx; acc.z = acc.z * fa + x.z * fx; acc.w = acc.w * fa + x.w * fx;
-  };
-  bool beside = false;
-#pragma unroll 1
+  // results of this row: first pieces, then those of CTAs, of its prefix (0) and of its own rows (1)
+  int n[2] = {0, 0}, c0[2], per[2], tile_row[2];
+#pragma unroll
   for (int side = 0; side < 2; ++side) {
+    if (side == 0 && g < 0) continue;
     const int e = side == 0 ? g : p.n_groups + s;
-    if (e < 0) continue;
     const int4 m = p.meta[e];
     if (m.y == 0) continue;
     const int row0 = side == 0 ? q_begin(p, p.group_cu ? __ldg(p.group_cu + g) : 0) : q_begin(p, s);
-    const int r = (row - row0) * p.G + hq - h * p.G, which = side == 0 ? 1 : 0;
+    const int r = (row - row0) * p.G + hq - h * p.G, front = m.w ? kItemMany : kItemFew, all = m.y + front;
     const int rts = m.w ? (m.z + kManyRows - 1) / kManyRows : 1, rt = m.w ? r / kManyRows : 0, run = m.w ? head.y : head.x;
-    const bool two = m.w && m.z - rt * kManyRows <= 128;   // each softmax group left a result
-    const int a = m.x + (h * rts + rt) * m.y, c0 = a / run, c1 = (a + m.y - 1) / run, cta0 = m.w ? 0 : head.z;
-    if (side == 1 && !beside && c0 == c1 && !m.w) return;  // whole, and nothing beside it: written where it was computed
-    beside = true;
-    const long long here = (long long)row * p.Hq + hq, of_all = (long long)p.n_q_rows * p.Hq;
-    add(which * of_all + here);
-    if (two) add((which + 2) * of_all + here);
-    for (int k = c0 + 1; k <= c1; ++k) {
-      const long long at = cut_part(p, cta0 + k) + r - rt * kManyRows;
-      add(at);
-      if (two) add(at + 128);
+    const int a = m.x + (h * rts + rt) * all;
+    c0[side] = (a + front) / run;
+    const int pieces = (a + all - 1) / run - c0[side] + 1;
+    if (side == 1 && n[0] == 0 && pieces == 1 && !m.w) return;                 // whole, and nothing beside it: written where it was computed
+    c0[side] += m.w ? 0 : head.z;
+    per[side] = m.w && m.z - rt * kManyRows <= 128 ? 2 : 1;                    // each softmax group left a result
+    n[side] = pieces * per[side];
+    tile_row[side] = r - rt * kManyRows;
+  }
+  const long long here = (long long)row * p.Hq + hq;
+  float top = -INFINITY, den = 0.f, acc[kV];
+#pragma unroll
+  for (int v = 0; v < kV; ++v) acc[v] = 0.f;
+  // a lane looks up one result of 32; what is not empty is added, the values of several on their way at a time
+  for (int i0 = 0; i0 < n[0] + n[1]; i0 += 32) {
+    const int i = i0 + lane;
+    long long at = 0;
+    float lse = -INFINITY;
+    if (i < n[0] + n[1]) {
+      const int side = i >= n[0], k = i - (side ? n[0] : 0), pc = side ? per[1] : per[0], piece = k / pc, second = k - piece * pc;
+      at = piece == 0 ? first_part(p, (side ? 0 : 1) + 2 * second) + here
+                      : cut_part(p, (side ? c0[1] : c0[0]) + piece) + (side ? tile_row[1] : tile_row[0]) + 128 * second;
+      lse = p.part[p.n_part * D + at];
+    }
+    float mx = fmaxf(lse, top);
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+    if (mx == -INFINITY) continue;
+    const float before = __expf(top - mx), w = __expf(lse - mx);               // (0 from -infinity)
+    top = mx;
+    den *= before;
+#pragma unroll
+    for (int v = 0; v < kV; ++v) acc[v] *= before;
+    const int count = min(32, n[0] + n[1] - i0);
+#pragma unroll 8
+    for (int k = 0; k < count; ++k) {
+      const float wk = __shfl_sync(0xffffffffu, w, k);
+      const long long ak = __shfl_sync(0xffffffffu, at, k);
+      if (wk == 0.f) continue;                             // (an empty one holds no values at all)
+      const float *x = p.part + ak * D + lane * kV;
+      den += wk;
+      if (kV == 4) {
+        const float4 f = __ldcs(reinterpret_cast<const float4 *>(x));
+        acc[0] = fmaf(wk, f.x, acc[0]); acc[1] = fmaf(wk, f.y, acc[1]); acc[2 % kV] = fmaf(wk, f.z, acc[2 % kV]); acc[3 % kV] = fmaf(wk, f.w, acc[3 % kV]);
+      } else {
+        const float2 f = __ldcs(reinterpret_cast<const float2 *>(x));
+        acc[0] = fmaf(wk, f.x, acc[0]); acc[1] = fmaf(wk, f.y, acc[1]);
+      }
     }
   }
   const float inv = den > 0.f ? 1.f / den : 0.f;
-  const size_t out = (size_t)u * D + c * 4;
-  if (p.out_f32) *reinterpret_cast<float4 *>(reinterpret_cast<float *>(p.o) + out) = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
-  else *reinterpret_cast<uint2 *>(reinterpret_cast<__nv_bfloat16 *>(p.o) + out) = make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
-  if (p.lse && c == 0) p.lse[u] = den > 0.f ? top + logf(den) : -INFINITY;
+#pragma unroll
+  for (int v = 0; v < kV; ++v) acc[v] *= inv;
+  const long long out = here * D + lane * kV;
+  if (p.out_f32) {
+    float *o = reinterpret_cast<float *>(p.o) + out;
+    if (kV == 4) *reinterpret_cast<float4 *>(o) = make_float4(acc[0], acc[1], acc[2 % kV], acc[3 % kV]);
+    else *reinterpret_cast<float2 *>(o) = make_float2(acc[0], acc[1]);
+  } else {
+    __nv_bfloat16 *o = reinterpret_cast<__nv_bfloat16 *>(p.o) + out;
+    if (kV == 4) *reinterpret_cast<uint2 *>(o) = make_uint2(pack_bf16(acc[0], acc[1]), pack_bf16(acc[2 % kV], acc[3 % kV]));
+    else *reinterpret_cast<uint32_t *>(o) = pack_bf16(acc[0], acc[1]);
+  }
+  if (p.lse && lane == 0) p.lse[here] = den > 0.f ? top + logf(den) : -INFINITY;
 }
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
@@ -1017,7 +1081,7 @@ ba_status ba_shared_prefix_attend(ba_ctx *ctx, const void *q, int32_t n_q_rows, 
   }
   const dim3 grid((unsigned)ctx->sm_count);
   const cudaStream_t cs = (cudaStream_t)stream;
-  const unsigned merge = (unsigned)(((long long)n_q_rows * p.Hq * (D / 4) + 255) / 256);
+  const unsigned merge = (unsigned)(((long long)n_q_rows * p.Hq + 7) / 8);
   if (D == 128) {
     BA_CUDA_TRY(ba_launch(ba_shared_attend_kernel<128>, grid, kThreads, SharedLayout<128>::kBytes, cs, true, tkx, tvx, tk, tv, p));
     BA_CUDA_TRY(ba_launch(ba_shared_merge_kernel<128>, dim3(merge), 256, 0, cs, true, p));
