@@ -169,12 +169,15 @@ def _load_marshal():
         return None
 
 
+_ROWS = {"ba_qk_norm_rope": (1, 2), "ba_qk_norm_rope_bwd": (1, 2, 10, 11), "ba_append_paged": (1, 2, 3)}
 _MAY_BE_NULL = {("ba_shared_prefix_attend", 6)}      # structures a call can do without: packed prefixes have no pages
 
 
 def _through_ctypes(name, *args):
     """A hot call whose arguments the extension does not take: through ctypes, like every other function of the library."""
     fn = getattr(load_library(), name)
+    if name in _ROWS:                                          # a tensor whose rows may lie apart stands for its address and stride
+        args = [x for i, a in enumerate(args) for x in (_rows(a, f"argument {i}") if i in _ROWS[name] else (a,))]
     given = [args[0]]
     for a, t in zip(args[1:], fn.argtypes[1:]):
         given.append(_ptr(a) if t is C.c_void_p else C.byref(a) if issubclass(t, C._Pointer) and not (a is None and (name, len(given)) in _MAY_BE_NULL) else a)
@@ -386,28 +389,19 @@ def _rows(t, what: str):
 
 def ba_qk_norm_rope(ctx, q, k, n_rows, pos, w_q, w_k, eps, q_out, k_out, stream=None):
     """q, k: [n_rows, heads, head_dim], rows may lie apart (views of a fused projection); None leaves a side out."""
-    q, q_stride = _rows(q, "q")
-    k, k_stride = _rows(k, "k")
-    _check(_calls().qk_norm_rope(ctx, q, q_stride, k, k_stride, n_rows, pos, w_q, w_k, eps, q_out, k_out, _stream_ptr(stream)),
+    _check(_calls().qk_norm_rope(ctx, q, k, n_rows, pos, w_q, w_k, eps, q_out, k_out, _stream_ptr(stream)),
            "ba_qk_norm_rope")
 
 
 def ba_qk_norm_rope_bwd(ctx, q, k, n_rows, pos, w_q, w_k, eps, dy_q, dy_k, dq, dk, dw_q, dw_k, grad_dtype, stream=None):
     """q, k, dq, dk: rows may lie apart; dw_q, dw_k: fp32 [head_dim], overwritten."""
-    q, q_stride = _rows(q, "q")
-    k, k_stride = _rows(k, "k")
-    dq, dq_stride = _rows(dq, "dq")
-    dk, dk_stride = _rows(dk, "dk")
-    _check(_calls().qk_norm_rope_bwd(ctx, q, q_stride, k, k_stride, n_rows, pos, w_q, w_k, eps, dy_q, dy_k, dq, dq_stride, dk, dk_stride,
+    _check(_calls().qk_norm_rope_bwd(ctx, q, k, n_rows, pos, w_q, w_k, eps, dy_q, dy_k, dq, dk,
                                      dw_q, dw_k, grad_dtype, _stream_ptr(stream)), "ba_qk_norm_rope_bwd")
 
 
 def ba_append_paged(ctx, q, k, v, n_rows, pos, w_q, w_k, eps, seq_cu, seq_start, n_seqs, q_out, k_pool, v_pool, pages, stream=None):
     """q (or None), k, v: rows may lie apart; seq_cu None: one row a sequence."""
-    q, q_stride = _rows(q, "q")
-    k, k_stride = _rows(k, "k")
-    v, v_stride = _rows(v, "v")
-    _check(_calls().append_paged(ctx, q, q_stride, k, k_stride, v, v_stride, n_rows, pos, w_q, w_k, eps, seq_cu, seq_start, n_seqs, q_out,
+    _check(_calls().append_paged(ctx, q, k, v, n_rows, pos, w_q, w_k, eps, seq_cu, seq_start, n_seqs, q_out,
                                  k_pool, v_pool, pages, _stream_ptr(stream)), "ba_append_paged")
 
 

@@ -137,6 +137,7 @@ ba_status ba_create(ba_ctx **out, const ba_config *cfg, int device, size_t works
   ctx->device = device;
   ctx->sm_count = prop.multiProcessorCount;
   ctx->scale = cfg->softmax_scale > 0.f ? cfg->softmax_scale : 1.0f / sqrtf((float)cfg->head_dim);
+  for (int m = 0; m < 64; ++m) ctx->turns[m] = m < cfg->head_dim / 2 ? pow(cfg->rope_theta, -2.0 * m / cfg->head_dim) / 6.283185307179586476925286766559 : 0.0;
   ctx->workspace_bytes = workspace_bytes;
   ctx->launches = 0;
   ctx->has_pending = 0;

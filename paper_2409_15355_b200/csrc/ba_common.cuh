@@ -105,6 +105,7 @@ struct ba_ctx {
   int device;
   int sm_count;
   float scale;              // softmax scale actually used
+  double turns[64];         // theta_m / (2 pi): what a position adds to the angle of rotary pair m, in turns
   void *workspace;          // device
   size_t workspace_bytes;
   int32_t *dev_status;      // device word: first non-zero ba_status recorded by a kernel

@@ -14,7 +14,7 @@
 
 #include "ba.h"
 
-static PyObject *s_data_ptr, *s_is_contiguous;
+static PyObject *s_data_ptr, *s_is_contiguous, *s_stride, *s_shape;
 static PyObject *other_way, *t_handle, *t_segments, *t_pages, *t_shared;
 /* bind()'s: the ctypes way, c_void_p, ba_segments, ba_page_table, ba_shared_batch */
 
@@ -78,13 +78,31 @@ static int to_size(PyObject *o, size_t *out) {
   *out = PyLong_AsSize_t(o);
   return *out == (size_t)-1 && PyErr_Occurred() ? unusual_if(PyExc_OverflowError) : 1;
 }
-static int to_int64(PyObject *o, int64_t *out) {
-  if (!PyLong_Check(o)) return UNUSUAL;
-  int overflow;
-  const long long v = PyLong_AsLongLongAndOverflow(o, &overflow);
-  if (overflow) return UNUSUAL;
-  *out = (int64_t)v;
-  return 1;
+/* A [rows, heads, head_dim] tensor whose rows may lie apart: its data and row stride (0: packed).  Anything else is the other way's. */
+static int to_rows(PyObject *o, void **out, int64_t *stride) {
+  *stride = 0;
+  if (o == Py_None || PyLong_Check(o)) return to_address(o, out);
+  PyObject *r = PyObject_CallMethodNoArgs(o, s_is_contiguous);
+  if (!r) return unusual_if(PyExc_AttributeError);
+  const int packed = PyObject_IsTrue(r);
+  Py_DECREF(r);
+  if (packed < 0) return 0;
+  if (!packed) {
+    PyObject *st = PyObject_CallMethodNoArgs(o, s_stride), *sh = st ? PyObject_GetAttr(o, s_shape) : NULL;
+    int k = UNUSUAL;
+    if (st && sh && PyTuple_Check(st) && PyTuple_Check(sh) && PyTuple_GET_SIZE(st) == 3 && PyTuple_GET_SIZE(sh) == 3) {
+      const long long s0 = PyLong_AsLongLong(PyTuple_GET_ITEM(st, 0)), s1 = PyLong_AsLongLong(PyTuple_GET_ITEM(st, 1));
+      if (PyLong_AsLongLong(PyTuple_GET_ITEM(st, 2)) == 1 && s1 == PyLong_AsLongLong(PyTuple_GET_ITEM(sh, 2)) && !PyErr_Occurred()) { *stride = s0; k = 1; }
+    }
+    Py_XDECREF(st); Py_XDECREF(sh);
+    PyErr_Clear();
+    if (k != 1) return k;
+  }
+  r = PyObject_CallMethodNoArgs(o, s_data_ptr);
+  if (!r) return unusual_if(PyExc_AttributeError);
+  const int k = PyLong_Check(r) ? from_int(r, out) : UNUSUAL;
+  Py_DECREF(r);
+  return k;
 }
 static int to_float(PyObject *o, float *out) {
   if (!PyFloat_Check(o)) return UNUSUAL;
@@ -116,7 +134,7 @@ static PyObject *go_other_way(const char *name, PyObject *const *args, Py_ssize_
 #define CTX ba_ctx *ctx; TAKE(to_context(args[0], &ctx))
 #define SEG(i, v) void *v; TAKE(to_memory(args[i], t_segments, sizeof(ba_segments), &v))
 #define PAGES(i, v) void *v; TAKE(to_memory(args[i], t_pages, sizeof(ba_page_table), &v))
-#define L(i, v) int64_t v; TAKE(to_int64(args[i], &v))
+#define R(i, v) void *v; int64_t v##_stride; TAKE(to_rows(args[i], &v, &v##_stride))
 #define F(i, v) float v; TAKE(to_float(args[i], &v))
 #define SHARED(i, v) void *v; TAKE(to_memory(args[i], t_shared, sizeof(ba_shared_batch), &v))
 #define CALL(expr)                                   \
@@ -179,19 +197,19 @@ static PyObject *m_final_attend_fused_paged(PyObject *self, PyObject *const *arg
 
 #define PRESENT(f) if (!p_##f || !t_shared) return go_other_way(function, args, nargs)
 static PyObject *m_qk_norm_rope(PyObject *self, PyObject *const *args, Py_ssize_t nargs) {
-  ARGS(ba_qk_norm_rope, 13); PRESENT(ba_qk_norm_rope); CTX; P(1, q); L(2, qs); P(3, k); L(4, ks); I(5, n); P(6, pos); P(7, wq); P(8, wk); F(9, eps);
-  P(10, q_out); P(11, k_out); P(12, stream);
-  CALL(p_ba_qk_norm_rope(ctx, q, qs, k, ks, n, pos, wq, wk, eps, q_out, k_out, stream));
+  ARGS(ba_qk_norm_rope, 11); PRESENT(ba_qk_norm_rope); CTX; R(1, q); R(2, k); I(3, n); P(4, pos); P(5, wq); P(6, wk); F(7, eps); P(8, q_out); P(9, k_out);
+  P(10, stream);
+  CALL(p_ba_qk_norm_rope(ctx, q, q_stride, k, k_stride, n, pos, wq, wk, eps, q_out, k_out, stream));
 }
 static PyObject *m_qk_norm_rope_bwd(PyObject *self, PyObject *const *args, Py_ssize_t nargs) {
-  ARGS(ba_qk_norm_rope_bwd, 20); PRESENT(ba_qk_norm_rope_bwd); CTX; P(1, q); L(2, qs); P(3, k); L(4, ks); I(5, n); P(6, pos); P(7, wq); P(8, wk);
-  F(9, eps); P(10, dyq); P(11, dyk); P(12, dq); L(13, dqs); P(14, dk); L(15, dks); P(16, dwq); P(17, dwk); I(18, type); P(19, stream);
-  CALL(p_ba_qk_norm_rope_bwd(ctx, q, qs, k, ks, n, pos, wq, wk, eps, dyq, dyk, dq, dqs, dk, dks, dwq, dwk, type, stream));
+  ARGS(ba_qk_norm_rope_bwd, 16); PRESENT(ba_qk_norm_rope_bwd); CTX; R(1, q); R(2, k); I(3, n); P(4, pos); P(5, wq); P(6, wk); F(7, eps); P(8, dyq); P(9, dyk);
+  R(10, dq); R(11, dk); P(12, dwq); P(13, dwk); I(14, type); P(15, stream);
+  CALL(p_ba_qk_norm_rope_bwd(ctx, q, q_stride, k, k_stride, n, pos, wq, wk, eps, dyq, dyk, dq, dq_stride, dk, dk_stride, dwq, dwk, type, stream));
 }
 static PyObject *m_append_paged(PyObject *self, PyObject *const *args, Py_ssize_t nargs) {
-  ARGS(ba_append_paged, 20); PRESENT(ba_append_paged); CTX; P(1, q); L(2, qs); P(3, k); L(4, ks); P(5, v); L(6, vs); I(7, n); P(8, pos); P(9, wq);
-  P(10, wk); F(11, eps); P(12, cu); P(13, start); I(14, n_seqs); P(15, q_out); P(16, kp); P(17, vp); PAGES(18, pages); P(19, stream);
-  CALL(p_ba_append_paged(ctx, q, qs, k, ks, v, vs, n, pos, wq, wk, eps, cu, start, n_seqs, q_out, kp, vp, pages, stream));
+  ARGS(ba_append_paged, 17); PRESENT(ba_append_paged); CTX; R(1, q); R(2, k); R(3, v); I(4, n); P(5, pos); P(6, wq); P(7, wk); F(8, eps); P(9, cu);
+  P(10, start); I(11, n_seqs); P(12, q_out); P(13, kp); P(14, vp); PAGES(15, pages); P(16, stream);
+  CALL(p_ba_append_paged(ctx, q, q_stride, k, k_stride, v, v_stride, n, pos, wq, wk, eps, cu, start, n_seqs, q_out, kp, vp, pages, stream));
 }
 static PyObject *m_shared_prefix_attend(PyObject *self, PyObject *const *args, Py_ssize_t nargs) {
   ARGS(ba_shared_prefix_attend, 15); PRESENT(ba_shared_prefix_attend); CTX; P(1, q); I(2, n); P(3, kx); P(4, vx); I(5, nx);
@@ -230,5 +248,7 @@ static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "ba_marshal", NULL, -
 PyMODINIT_FUNC PyInit_ba_marshal(void) {
   s_data_ptr = PyUnicode_InternFromString("data_ptr");
   s_is_contiguous = PyUnicode_InternFromString("is_contiguous");
-  return s_data_ptr && s_is_contiguous ? PyModule_Create(&module) : NULL;
+  s_stride = PyUnicode_InternFromString("stride");
+  s_shape = PyUnicode_InternFromString("shape");
+  return s_data_ptr && s_is_contiguous && s_stride && s_shape ? PyModule_Create(&module) : NULL;
 }
