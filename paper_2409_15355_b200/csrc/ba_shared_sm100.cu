@@ -16,8 +16,8 @@
 // Few rows: warp 8 asks the copy engine for key and value tiles (a ring of stages, one box per page); warps 0-7 take 16 keys of a tile
 // each, with mma.sync on operands from shared memory: S = Q K^T, softmax with maxima and sums of the warp's own keys, O += P V with P from
 // registers.  The warps share nothing until the end of a piece, where their maxima, sums and accumulators are merged.
-// Many rows: tcgen05 with accumulators in tensor memory, warps 0-3 and 4-7 softmax (a thread a row), warp 8 copies, warp 9 issues the
-// products, warps 10-11 fetch queries.  Items of more than 128 rows: the two softmax groups have a tile of queries each and share key
+// Many rows: tcgen05 with accumulators in tensor memory, warps 0-3 and 4-7 softmax (a thread a row), warps 8 and 10 copy keys
+// and values, warp 9 issues the products, warp 11 fetches queries.  Items of more than 128 rows: the two softmax groups have a tile of queries each and share key
 // tiles; items of fewer: they share the query tile and take key tiles in turn, each with an accumulator of its own, so that products and
 // exponentials overlap there too; the merge counts them as two results.
 //
@@ -43,9 +43,12 @@ constexpr int kConsumerRegs = 224, kCopyRegs = 56;
 constexpr int kMaxEntries = BA_SHARED_MAX;
 constexpr int kSoftmaxRegs = 208, kServiceRegs = 88;     // of CTAs for many rows: 256 * 208 + 128 * 88
 // What a key tile costs, to share out the CTAs: two query tiles, one, and few rows (cycles / 1000).
-// Units that an item counts for besides its key tiles: what begins and ends it (queries, the pipeline's filling, the rows' way out).
-constexpr int kItemMany = 3, kItemFew = 1;
-constexpr double kCostPair = 4., kCostSolo = 3., kCostFew = 3.;
+// Units of the streams.  A key tile counts for one in the stream of few rows and, in the other, for three with two query tiles and two with
+// one; an item counts besides for what begins and ends it (queries, the pipeline's filling, the rows' way out).
+constexpr int kTileFew = 1, kTilePair = 3, kTileSolo = 2, kFrontFew = 4, kFrontMany = 10;
+// What a unit costs, to share out the CTAs between the streams.
+constexpr float kCostFew = 3.f, kCostMany = 2.f;
+constexpr int kMostUnits = INT32_MAX / kThreads;           // of one thread's entries: the sums stay in 32 bits
 constexpr float kRescale = 8.f;       // O is rescaled when a maximum grows by more than 2^8: exact in real arithmetic, values stay bounded
 
 struct SharedParams {
@@ -54,6 +57,7 @@ struct SharedParams {
   float *lse;
   int32_t *status;
   int out_f32, Hq, Hkv, G;
+  int q_boxes;                        // 128 is a multiple of G: the copy engine fetches query tiles
   float scale_log2;
   int n_q_rows, batch, n_groups;
   const int32_t *group_cu, *prefix_cu, *q_cu, *own_len;
@@ -68,7 +72,7 @@ struct SharedParams {
   int4 *meta;                         // [n_groups + batch]: first unit in its stream, tiles, rows, many; then runs of the two kinds, CTAs for many, validity
 };
 
-constexpr int kCtrlBytes = 1088;
+constexpr int kCtrlBytes = 1360;
 
 template <int D>
 struct SharedLayout {
@@ -94,12 +98,13 @@ static_assert(SharedLayout<128>::kBytes <= 227 * 1024, "shared memory");
 
 struct SharedCtrl {
   uint64_t full[10], empty[10];       // few: the ring
-  uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4];                       // many
+  uint64_t k_full[5], k_empty[5], v_full[4], v_empty[4];                       // many
   uint64_t q_full, q_empty, s_full[2], p_full[2][2], o_done[2], o_free[2];
   int abort_flag, invalid;
   uint32_t tmem_base;
   uint32_t alone[kMaxEntries / 32];   // a bit an entry: own rows of a sequence without prefix
-  double warp_units[2][kThreads / 32], warp_cost[kThreads / 32];
+  uint32_t pairs[kMaxEntries / 32];   // a bit an entry: it has items of more than 128 rows
+  int2 warp_sums[kThreads / 32];      // units of few rows, of many
 };
 static_assert(sizeof(SharedCtrl) <= kCtrlBytes, "control area");
 
@@ -140,11 +145,20 @@ __device__ __forceinline__ bool load_entry(const SharedParams &p, int e, Entry &
 }
 __device__ __forceinline__ int tiles_of(const Entry &x) { return (x.len + kTile - 1) / kTile; }
 __device__ __forceinline__ bool is_many(const SharedParams &p, const Entry &x) { return x.rows * p.G > kRows; }
-__device__ __forceinline__ int row_tiles_of(const SharedParams &p, const Entry &x) { return is_many(p, x) ? (x.rows * p.G + kManyRows - 1) / kManyRows : x.rows > 0; }
-__device__ __forceinline__ int item_units(const SharedParams &p, const Entry &x) {
-  const int tiles = tiles_of(x);
-  return tiles > 0 ? tiles + (is_many(p, x) ? kItemMany : kItemFew) : 0;
-}
+// Units of a tile of an item of n rows.
+__device__ __forceinline__ int tile_units(bool many, int n_rows) { return !many ? kTileFew : n_rows > 128 ? kTilePair : kTileSolo; }
+// How an entry's items lie in its stream: head by head, row tile by row tile, each `front` units and those of its tiles.
+struct Lay {
+  int tiles, rts, front, full, last;   // row tiles; units of an item that is not a head's last one, and of one that is
+  __device__ __forceinline__ Lay(int tiles_, int rows, bool many) : tiles(tiles_) {
+    rts = many ? (rows + kManyRows - 1) / kManyRows : rows > 0;
+    front = many ? kFrontMany : kFrontFew;
+    full = front + tiles * tile_units(many, kManyRows);
+    last = front + tiles * tile_units(many, rows - (rts - 1) * kManyRows);
+  }
+  __device__ __forceinline__ long long a_head() const { return tiles > 0 && rts > 0 ? (long long)(rts - 1) * full + last : 0; }
+};
+__device__ __forceinline__ Lay lay_of(const SharedParams &p, const Entry &x) { return Lay(tiles_of(x), x.rows * p.G, is_many(p, x)); }
 // Rows of an item: row r is head h of token tok of its queries (tok x heads + h) from `at` on.
 struct RowMap {
   long long at;         // of its first token and head, as o is indexed without the head's values
@@ -190,14 +204,17 @@ __device__ __forceinline__ Piece piece_at(const SharedParams &p, const int *unit
   k.e = last_at_most(units, n_entries, at);
   k.x = get_entry(p, k.e);
   k.tiles = tiles_of(k.x);
-  const int item_all = item_units(p, k.x), front = item_all - k.tiles, begin = units[k.e];
-  const int item = (at - begin) / item_all, rts = row_tiles_of(p, k.x), from = at - begin - item * item_all;
-  k.head = item / rts; k.row0 = (item - k.head * rts) * kManyRows;
+  const Lay lay = lay_of(p, k.x);
+  const int a_head = (int)lay.a_head(), local = at - units[k.e];
+  k.head = local / a_head;
+  const int in_head = local - k.head * a_head, rt = min(in_head / lay.full, lay.rts - 1), from = in_head - rt * lay.full;
+  k.row0 = rt * kManyRows;
   k.n_rows = min(kManyRows, k.x.rows * p.G - k.row0);
-  const int to = min(item_all, from + end - at);
+  const int to = min(rt + 1 < lay.rts ? lay.full : lay.last, from + end - at), w = tile_units(is_many(p, k.x), k.n_rows);
   k.units = to - from;
-  k.tile0 = max(0, from - front);
-  k.n = max(0, to - front) - k.tile0;
+  // tile t is worked on where its first unit lies
+  k.tile0 = max(0, from - lay.front + w - 1) / w;
+  k.n = max(0, to - lay.front + w - 1) / w - k.tile0;
   return k;
 }
 // Where the keys of a piece lie.  Lane i of the copying warp has box i of a tile, a box per page.
@@ -259,22 +276,17 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 }
 __device__ __forceinline__ void consumers_sync() { asm volatile("bar.sync 1, %0;" ::"n"(32 * kWarps) : "memory"); }
 
-// One piece of an item of few rows: the consumer warps' work.  Moves the ring position on.
+// Queries of a piece of an item of few rows as the A operand, straight from memory (rows past the item's are zeros), and how many
+// keys the lane's two rows see.
 template <int D>
-__device__ __forceinline__ void consume_piece(const SharedParams &p, const Piece &k, uint8_t *smem, SharedCtrl *ctrl, int &ring, bool &ok, bool direct) {
-  using L = SharedLayout<D>;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, quad = lane >> 2, in_quad = lane & 3;
-  volatile int *abort_flag = &ctrl->abort_flag;
+__device__ __forceinline__ void load_queries(const SharedParams &p, const Piece &k, uint32_t (&qa)[D / 16][4], int (&limit)[2]) {
+  const int lane = threadIdx.x & 31, quad = lane >> 2, in_quad = lane & 3;
   const bool own = k.e >= p.n_groups;
-  const int n_rows = k.n_rows;
   const RowMap map(p, k.x, 0, k.head);
-  // queries as the A operand, straight from memory; rows past the item's are zeros
-  uint32_t qa[D / 16][4];
-  int limit[2];                          // keys that the lane's rows see
 #pragma unroll
   for (int hi = 0; hi < 2; ++hi) {
     const int r = hi * 8 + quad;
-    const bool there = r < n_rows;
+    const bool there = r < k.n_rows;
     const uint32_t *src = reinterpret_cast<const uint32_t *>(p.q + map.row(there ? r : 0) * D) + in_quad;
     limit[hi] = own ? k.x.len - (k.x.rows - 1 - map.token(there ? r : 0)) : k.x.len;
 #pragma unroll
@@ -283,154 +295,199 @@ __device__ __forceinline__ void consume_piece(const SharedParams &p, const Piece
       qa[c][hi + 2] = there ? __ldg(src + c * 8 + 4) : 0u;
     }
   }
-  float o[D / 8][4], mx[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f};
-#pragma unroll
-  for (int c = 0; c < D / 8; ++c) o[c][0] = o[c][1] = o[c][2] = o[c][3] = 0.f;
-  const float sl = p.scale_log2;
-  const int k_row = warp * 16 + ((lane >> 4) & 1) * 8 + (lane & 7), k_col = (lane >> 3) & 1;
-  const int v_row = warp * 16 + ((lane >> 3) & 1) * 8 + (lane & 7), v_col = (lane >> 4) & 1;
-  for (int j = 0; j < k.n; ++j, ring += 2) {
-    const int key0 = (k.tile0 + j) * kTile + warp * 16;    // this warp's keys
-    const int left = k.x.len - key0;
-    const int ks = ring % L::kStages, vs = (ring + 1) % L::kStages;
-    if (ok) ok = mbar_wait(&ctrl->full[ks], (ring / L::kStages) & 1, abort_flag);
-    ok = __all_sync(0xffffffffu, ok);
-    float s[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-    if (ok && left > 0) {
-      const uint32_t tile = smem_u32(smem + ks * L::kTileBytes) + k_row * 128;
-#pragma unroll
-      for (int c = 0; c < D / 16; ++c) {
-        uint32_t b[4];
-        const int col = c * 2 + k_col;
-        ldsm4(b, tile + (col >> 3) * L::kRegion + (((col & 7) ^ (k_row & 7)) << 4));
-        mma_16816(s[0], qa[c], b[0], b[1]);
-        mma_16816(s[1], qa[c], b[2], b[3]);
-      }
+}
+
+// The pieces of a run of few rows, one by one: the consumer warps' view of it.
+struct FewRun {
+  const int *units;
+  int n_entries, at, end;
+  __device__ __forceinline__ bool next(const SharedParams &p, Piece &k) {
+    while (at < end) {
+      k = piece_at(p, units, n_entries, at, end);
+      at += k.units;
+      if (k.n > 0) return true;
     }
-    __syncwarp();
-    if (lane == 0) mbar_arrive(&ctrl->empty[ks]);
-    uint32_t pa[4];
-    if (ok && left > 0) {
-      float top[2];
+    return false;
+  }
+};
+
+// The consumer warps' work on a run of few rows.
+template <int D>
+__device__ __forceinline__ void consume_run(const SharedParams &p, FewRun run, uint8_t *smem, SharedCtrl *ctrl) {
+  using L = SharedLayout<D>;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, quad = lane >> 2, in_quad = lane & 3;
+  volatile int *abort_flag = &ctrl->abort_flag;
+  int ring = 0;
+  bool ok = true;
+  uint32_t qa[D / 16][4];
+  int limit[2];
+  Piece k;
+  bool more = run.next(p, k);
+  if (more) load_queries<D>(p, k, qa, limit);
+  while (more) {                         // (to the end even after a wait that expired: the warps meet at barriers)
+    const bool own = k.e >= p.n_groups;
+    const bool direct = own && k.n == k.tiles && (ctrl->alone[k.e >> 5] >> (k.e & 31) & 1);
+    const int n_rows = k.n_rows;
+    float o[D / 8][4], mx[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f};
 #pragma unroll
-      for (int hi = 0; hi < 2; ++hi) {
-        if (key0 + 16 > limit[hi]) {
+    for (int c = 0; c < D / 8; ++c) o[c][0] = o[c][1] = o[c][2] = o[c][3] = 0.f;
+    const float sl = p.scale_log2;
+    const int k_row = warp * 16 + ((lane >> 4) & 1) * 8 + (lane & 7), k_col = (lane >> 3) & 1;
+    const int v_row = warp * 16 + ((lane >> 3) & 1) * 8 + (lane & 7), v_col = (lane >> 4) & 1;
+    for (int j = 0; j < k.n; ++j, ring += 2) {
+      const int key0 = (k.tile0 + j) * kTile + warp * 16;    // this warp's keys
+      const int left = k.x.len - key0;
+      const int ks = ring % L::kStages, vs = (ring + 1) % L::kStages;
+      if (ok) ok = mbar_wait(&ctrl->full[ks], (ring / L::kStages) & 1, abort_flag);
+      ok = __all_sync(0xffffffffu, ok);
+      float s[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+      if (ok && left > 0) {
+        const uint32_t tile = smem_u32(smem + ks * L::kTileBytes) + k_row * 128;
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (key0 + (i >> 1) * 8 + in_quad * 2 + (i & 1) >= limit[hi]) s[i >> 1][hi * 2 + (i & 1)] = -INFINITY;
+        for (int c = 0; c < D / 16; ++c) {
+          uint32_t b[4];
+          const int col = c * 2 + k_col;
+          ldsm4(b, tile + (col >> 3) * L::kRegion + (((col & 7) ^ (k_row & 7)) << 4));
+          mma_16816(s[0], qa[c], b[0], b[1]);
+          mma_16816(s[1], qa[c], b[2], b[3]);
         }
-        top[hi] = fmaxf(fmaxf(s[0][hi * 2], s[0][hi * 2 + 1]), fmaxf(s[1][hi * 2], s[1][hi * 2 + 1]));
-        top[hi] = fmaxf(top[hi], __shfl_xor_sync(0xffffffffu, top[hi], 1));
-        top[hi] = fmaxf(top[hi], __shfl_xor_sync(0xffffffffu, top[hi], 2));
-        top[hi] = fmaxf(top[hi], mx[hi]);
       }
-      // (from -inf: yes, unless nothing has been seen yet)
-      const bool grow = (top[0] > mx[0] && !((top[0] - mx[0]) * sl <= kRescale)) || (top[1] > mx[1] && !((top[1] - mx[1]) * sl <= kRescale));
-      if (__any_sync(0xffffffffu, grow)) {
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&ctrl->empty[ks]);
+      uint32_t pa[4];
+      if (ok && left > 0) {
+        float top[2];
 #pragma unroll
         for (int hi = 0; hi < 2; ++hi) {
-          const float alpha = mx[hi] == -INFINITY ? 0.f : ex2((mx[hi] - top[hi]) * sl);     // (nothing summed so far)
-          mx[hi] = top[hi];
-          sum[hi] *= alpha;
+          if (key0 + 16 > limit[hi]) {
 #pragma unroll
-          for (int c = 0; c < D / 8; ++c) { o[c][hi * 2] *= alpha; o[c][hi * 2 + 1] *= alpha; }
+            for (int i = 0; i < 4; ++i)
+              if (key0 + (i >> 1) * 8 + in_quad * 2 + (i & 1) >= limit[hi]) s[i >> 1][hi * 2 + (i & 1)] = -INFINITY;
+          }
+          top[hi] = fmaxf(fmaxf(s[0][hi * 2], s[0][hi * 2 + 1]), fmaxf(s[1][hi * 2], s[1][hi * 2 + 1]));
+          top[hi] = fmaxf(top[hi], __shfl_xor_sync(0xffffffffu, top[hi], 1));
+          top[hi] = fmaxf(top[hi], __shfl_xor_sync(0xffffffffu, top[hi], 2));
+          top[hi] = fmaxf(top[hi], mx[hi]);
+        }
+        // (from -inf: yes, unless nothing has been seen yet)
+        const bool grow = (top[0] > mx[0] && !((top[0] - mx[0]) * sl <= kRescale)) || (top[1] > mx[1] && !((top[1] - mx[1]) * sl <= kRescale));
+        if (__any_sync(0xffffffffu, grow)) {
+#pragma unroll
+          for (int hi = 0; hi < 2; ++hi) {
+            const float alpha = mx[hi] == -INFINITY ? 0.f : ex2((mx[hi] - top[hi]) * sl);     // (nothing summed so far)
+            mx[hi] = top[hi];
+            sum[hi] *= alpha;
+#pragma unroll
+            for (int c = 0; c < D / 8; ++c) { o[c][hi * 2] *= alpha; o[c][hi * 2 + 1] *= alpha; }
+          }
+        }
+#pragma unroll
+        for (int hi = 0; hi < 2; ++hi) {
+          const float neg = mx[hi] == -INFINITY ? 0.f : -mx[hi] * sl;
+          float e[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) e[i] = ex2(fmaf(s[i >> 1][hi * 2 + (i & 1)], sl, neg));
+          sum[hi] += (e[0] + e[1]) + (e[2] + e[3]);
+          pa[hi] = pack_bf16(e[0], e[1]);
+          pa[hi + 2] = pack_bf16(e[2], e[3]);
         }
       }
-#pragma unroll
-      for (int hi = 0; hi < 2; ++hi) {
-        const float neg = mx[hi] == -INFINITY ? 0.f : -mx[hi] * sl;
-        float e[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) e[i] = ex2(fmaf(s[i >> 1][hi * 2 + (i & 1)], sl, neg));
-        sum[hi] += (e[0] + e[1]) + (e[2] + e[3]);
-        pa[hi] = pack_bf16(e[0], e[1]);
-        pa[hi + 2] = pack_bf16(e[2], e[3]);
-      }
-    }
-    if (ok) ok = mbar_wait(&ctrl->full[vs], ((ring + 1) / L::kStages) & 1, abort_flag);
-    ok = __all_sync(0xffffffffu, ok);
-    if (ok && left > 0) {
-      uint8_t *tile = smem + vs * L::kTileBytes;
-      if (left < 16) {
-        // values behind the end may be anything, and zero times a NaN is a NaN
-        for (int i = lane; i < (16 - left) * (D / 8); i += 32) {
-          const int row = warp * 16 + left + i / (D / 8), col = i % (D / 8);
-          *reinterpret_cast<uint4 *>(tile + (col >> 3) * L::kRegion + row * 128 + ((col & 7) << 4)) = make_uint4(0, 0, 0, 0);
+      if (ok) ok = mbar_wait(&ctrl->full[vs], ((ring + 1) / L::kStages) & 1, abort_flag);
+      ok = __all_sync(0xffffffffu, ok);
+      if (ok && left > 0) {
+        uint8_t *tile = smem + vs * L::kTileBytes;
+        if (left < 16) {
+          // values behind the end may be anything, and zero times a NaN is a NaN
+          for (int i = lane; i < (16 - left) * (D / 8); i += 32) {
+            const int row = warp * 16 + left + i / (D / 8), col = i % (D / 8);
+            *reinterpret_cast<uint4 *>(tile + (col >> 3) * L::kRegion + row * 128 + ((col & 7) << 4)) = make_uint4(0, 0, 0, 0);
+          }
+          fence_proxy_async();                               // (the copy engine writes the stage next)
+          __syncwarp();
         }
-        fence_proxy_async();                               // (the copy engine writes the stage next)
-        __syncwarp();
+        const uint32_t base = smem_u32(tile) + v_row * 128;
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c) {
+          uint32_t b[4];
+          const int col = c * 2 + v_col;
+          ldsm4_t(b, base + (col >> 3) * L::kRegion + (((col & 7) ^ (v_row & 7)) << 4));
+          mma_16816(o[2 * c], pa, b[0], b[1]);
+          mma_16816(o[2 * c + 1], pa, b[2], b[3]);
+        }
       }
-      const uint32_t base = smem_u32(tile) + v_row * 128;
-#pragma unroll
-      for (int c = 0; c < D / 16; ++c) {
-        uint32_t b[4];
-        const int col = c * 2 + v_col;
-        ldsm4_t(b, base + (col >> 3) * L::kRegion + (((col & 7) ^ (v_row & 7)) << 4));
-        mma_16816(o[2 * c], pa, b[0], b[1]);
-        mma_16816(o[2 * c + 1], pa, b[2], b[3]);
-      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&ctrl->empty[vs]);
     }
-    __syncwarp();
-    if (lane == 0) mbar_arrive(&ctrl->empty[vs]);
-  }
-  // The warps' results: rows' maxima and sums are exchanged, every accumulator is scaled to the common maximum and divided by the
-  // common sum, and the eight are added 64 columns at a time.
-  float2 *stat = reinterpret_cast<float2 *>(smem + L::kStat);
-  float *buf = reinterpret_cast<float *>(smem + L::kBuf);
+    // the next piece's queries are on their way while this one is finished
+    const Piece done = k;
+    more = run.next(p, k);
+    if (more) load_queries<D>(p, k, qa, limit);
+    // The warps' results: rows' maxima and sums are exchanged, every accumulator is scaled to the common maximum and divided by the
+    // common sum, and the eight are added 64 columns at a time.
+    const RowMap map(p, done.x, 0, done.head);
+    float2 *stat = reinterpret_cast<float2 *>(smem + L::kStat);
+    float *buf = reinterpret_cast<float *>(smem + L::kBuf);
 #pragma unroll
-  for (int hi = 0; hi < 2; ++hi) {
-    sum[hi] += __shfl_xor_sync(0xffffffffu, sum[hi], 1);
-    sum[hi] += __shfl_xor_sync(0xffffffffu, sum[hi], 2);
-    if (in_quad == 0) stat[warp * kRows + hi * 8 + quad] = make_float2(mx[hi], sum[hi]);
-  }
-  consumers_sync();
-  // a row's place: in the output, among the first pieces, or in the CTA's own
-  auto place = [&](int r) -> long long {
-    return direct ? map.row(r) : k.tile0 == 0 ? first_part(p, own ? 0 : 1) + map.row(r) : cut_part(p, (int)blockIdx.x) + r;
-  };
-  float f[2];
-#pragma unroll
-  for (int hi = 0; hi < 2; ++hi) {
-    const int r = hi * 8 + quad;
-    float top = -INFINITY, den = 0.f;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) top = fmaxf(top, stat[w * kRows + r].x);
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
-      const float2 v = stat[w * kRows + r];
-      if (v.x != -INFINITY) den += v.y * ex2((v.x - top) * sl);
+    for (int hi = 0; hi < 2; ++hi) {
+      sum[hi] += __shfl_xor_sync(0xffffffffu, sum[hi], 1);
+      sum[hi] += __shfl_xor_sync(0xffffffffu, sum[hi], 2);
+      if (in_quad == 0) stat[warp * kRows + hi * 8 + quad] = make_float2(mx[hi], sum[hi]);
     }
-    f[hi] = mx[hi] != -INFINITY && den > 0.f ? ex2((mx[hi] - top) * sl) / den : 0.f;
-    if (ok && warp == 0 && in_quad == 0 && r < n_rows) {
-      const float lse = den > 0.f ? (top * sl + log2f(den)) * 0.6931471805599453f : -INFINITY;
-      if (!direct) p.part[p.n_part * D + place(r)] = lse;
-      else if (p.lse) p.lse[place(r)] = lse;
-    }
-  }
-#pragma unroll
-  for (int half = 0; half < D / 64; ++half) {
-    float *mine = buf + warp * 16 * L::kBufStride;
-#pragma unroll
-    for (int c = 0; c < 8; ++c)
-#pragma unroll
-      for (int hi = 0; hi < 2; ++hi)
-        *reinterpret_cast<float2 *>(mine + (hi * 8 + quad) * L::kBufStride + c * 8 + in_quad * 2) =
-            make_float2(o[half * 8 + c][hi * 2] * f[hi], o[half * 8 + c][hi * 2 + 1] * f[hi]);
     consumers_sync();
-    const int r = threadIdx.x >> 4, col = (threadIdx.x & 15) * 4;
-    if (ok && r < n_rows) {
-      float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
+    // a row's place: in the output, among the first pieces, or in the CTA's own
+    auto place = [&](int r) -> long long {
+      return direct ? map.row(r) : done.tile0 == 0 ? first_part(p, own ? 0 : 1) + map.row(r) : cut_part(p, (int)blockIdx.x) + r;
+    };
+    float f[2];
+#pragma unroll
+    for (int hi = 0; hi < 2; ++hi) {
+      const int r = hi * 8 + quad;
+      float top = -INFINITY, den = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) top = fmaxf(top, stat[w * kRows + r].x);
 #pragma unroll
       for (int w = 0; w < kWarps; ++w) {
-        const float4 v = *reinterpret_cast<const float4 *>(buf + (w * 16 + r) * L::kBufStride + col);
-        t.x += v.x; t.y += v.y; t.z += v.z; t.w += v.w;
+        const float2 v = stat[w * kRows + r];
+        if (v.x != -INFINITY) den += v.y * ex2((v.x - top) * sl);
       }
-      const long long at = place(r) * D + half * 64 + col;
-      if (!direct) *reinterpret_cast<float4 *>(p.part + at) = t;
-      else if (p.out_f32) *reinterpret_cast<float4 *>(reinterpret_cast<float *>(p.o) + at) = t;
-      else *reinterpret_cast<uint2 *>(reinterpret_cast<__nv_bfloat16 *>(p.o) + at) = make_uint2(pack_bf16(t.x, t.y), pack_bf16(t.z, t.w));
+      f[hi] = mx[hi] != -INFINITY && den > 0.f ? ex2((mx[hi] - top) * sl) / den : 0.f;
+      if (ok && warp == 0 && in_quad == 0 && r < n_rows) {
+        const float lse = den > 0.f ? (top * sl + log2f(den)) * 0.6931471805599453f : -INFINITY;
+        if (!direct) p.part[p.n_part * D + place(r)] = lse;
+        else if (p.lse) p.lse[place(r)] = lse;
+      }
     }
-    consumers_sync();
+    // up to eight rows: the buffer's other eight rows take the other 64 columns, and one round does
+    const bool compact = n_rows <= 8;
+    float *mine = buf + warp * 16 * L::kBufStride;
+    const int r16 = threadIdx.x >> 4, col = (threadIdx.x & 15) * 4;
+#pragma unroll
+    for (int half = 0; half < D / 64; ++half) {
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        *reinterpret_cast<float2 *>(mine + ((compact ? half * 8 : 0) + quad) * L::kBufStride + c * 8 + in_quad * 2) =
+            make_float2(o[half * 8 + c][0] * f[0], o[half * 8 + c][1] * f[0]);
+        if (!compact)
+          *reinterpret_cast<float2 *>(mine + (8 + quad) * L::kBufStride + c * 8 + in_quad * 2) =
+              make_float2(o[half * 8 + c][2] * f[1], o[half * 8 + c][3] * f[1]);
+      }
+      if (compact && half + 1 < D / 64) continue;
+      consumers_sync();
+      const int r = compact ? r16 & 7 : r16, h = compact ? r16 >> 3 : half;
+      if (ok && r < n_rows && h < D / 64) {
+        float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+          const float4 v = *reinterpret_cast<const float4 *>(buf + (w * 16 + r16) * L::kBufStride + col);
+          t.x += v.x; t.y += v.y; t.z += v.z; t.w += v.w;
+        }
+        const long long at = place(r) * D + h * 64 + col;
+        if (!direct) *reinterpret_cast<float4 *>(p.part + at) = t;
+        else if (p.out_f32) *reinterpret_cast<float4 *>(reinterpret_cast<float *>(p.o) + at) = t;
+        else *reinterpret_cast<uint2 *>(reinterpret_cast<__nv_bfloat16 *>(p.o) + at) = make_uint2(pack_bf16(t.x, t.y), pack_bf16(t.z, t.w));
+      }
+      consumers_sync();
+    }
   }
 }
 
@@ -444,7 +501,9 @@ __device__ __forceinline__ void few_rows(const SharedParams &p, const CUtensorMa
   bool ok = true;
   if (warp >= kWarps) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kCopyRegs));
-    if (warp == kWarps) {
+    if (warp < kWarps + 2) {
+      const int kv = warp - kWarps;                        // keys and values are asked for by a warp each: a tile is up to 16 boxes
+      ring = kv;
       for (int at = begin; at < end && ok;) {
         const Piece k = piece_at(p, units, n_entries, at, end);
         at += k.units;
@@ -455,31 +514,23 @@ __device__ __forceinline__ void few_rows(const SharedParams &p, const CUtensorMa
         for (int j = 0; j < k.n && ok; ++j) {
           const int row = next;
           if (j + 1 < k.n) next = box_row(p, src, k.tile0 + j + 1);
-          for (int kv = 0; kv < 2; ++kv, ++ring) {
-            const int stage = ring % L::kStages;
-            ok = mbar_wait(&ctrl->empty[stage], ((ring / L::kStages) & 1) ^ 1, &ctrl->abort_flag);
-            ok = __all_sync(0xffffffffu, ok);
-            if (!ok) break;
-            copy_tile<D>(src, own ? (kv ? tmap_v : tmap_k) : (kv ? tmap_vx : tmap_kx), smem + stage * L::kTileBytes, &ctrl->full[stage], k.head, row);
-          }
+          const int stage = ring % L::kStages;
+          ok = __all_sync(0xffffffffu, mbar_wait(&ctrl->empty[stage], ((ring / L::kStages) & 1) ^ 1, &ctrl->abort_flag));
+          if (!ok) break;
+          copy_tile<D>(src, own ? (kv ? tmap_v : tmap_k) : (kv ? tmap_vx : tmap_kx), smem + stage * L::kTileBytes, &ctrl->full[stage], k.head, row);
+          ring += 2;
         }
       }
       if (!ok) {
         // leave no copy in flight: wait (bounded) for the tiles already requested
-        for (int i = max(0, ring - L::kStages); i < ring; ++i)
+        for (int i = max(kv, ring - 2 * ((L::kStages + 1) / 2)); i < ring; i += 2)
           for (uint32_t spin = 0; spin < (1u << 20); ++spin)
             if (mbar_try_wait(&ctrl->full[i % L::kStages], (i / L::kStages) & 1)) break;
       }
     }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kConsumerRegs));
-    for (int at = begin; at < end;) {                      // (to the end even after a wait that expired: the warps meet at barriers)
-      const Piece k = piece_at(p, units, n_entries, at, end);
-      at += k.units;
-      if (k.n == 0) continue;
-      const bool direct = k.e >= p.n_groups && k.n == k.tiles && (ctrl->alone[k.e >> 5] >> (k.e & 31) & 1);
-      consume_piece<D>(p, k, smem, ctrl, ring, ok, direct);
-    }
+    consume_run<D>(p, {units, n_entries, begin, end}, smem, ctrl);
   }
 }
 
@@ -492,57 +543,58 @@ __device__ __forceinline__ void copy_16_or_zero(uint32_t dst, const void *src, b
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
 }
 
+// The ring of key tiles of a CTA for many rows.  The second query tile's place is one more stage where the run has no pairs: a stage is
+// refilled once its product is done and needed one softmax later, which HBM under load outlasts (160 requests in seven groups: the CTAs for
+// many rows waited 1500 of 6500 cycles for keys).
+template <int D>
+struct KeyRing {
+  using L = SharedLayout<D>;
+  bool deep;
+  __device__ __forceinline__ int stage(int i) const { return deep ? i % (L::kDepth + 1) : i % L::kDepth; }
+  __device__ __forceinline__ int phase(int i) const { return (deep ? i / (L::kDepth + 1) : i / L::kDepth) & 1; }
+  __device__ __forceinline__ int depth() const { return L::kDepth + (deep ? 1 : 0); }
+  static __device__ __forceinline__ int offset(int stage) { return stage < L::kDepth ? L::kKeys + stage * L::kTileBytes : L::kTileBytes; }
+};
+
 // A CTA for many rows: units [begin, end) of that stream.  Softmax group t has, of the n key tiles of a piece, all (a piece of more
 // than 128 rows: pair) or t, t + 2, ..
 template <int D>
 __device__ __forceinline__ void many_rows(const SharedParams &p, const CUtensorMap *tmap_kx, const CUtensorMap *tmap_vx, const CUtensorMap *tmap_k,
-                                          const CUtensorMap *tmap_v, uint8_t *smem, SharedCtrl *ctrl, const int *units, int n_entries, int begin, int end) {
+                                          const CUtensorMap *tmap_v, const CUtensorMap *tmap_q, uint8_t *smem, SharedCtrl *ctrl, const int *units,
+                                         int n_entries, int begin, int end) {
   using L = SharedLayout<D>;
   constexpr int kDepth = L::kDepth;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t tmem = ctrl->tmem_base;
   volatile int *abort_flag = &ctrl->abort_flag;
   uint64_t *k_full = ctrl->k_full, *v_full = ctrl->v_full, *k_empty = ctrl->k_empty, *v_empty = ctrl->v_empty;
-  bool ok = true;
+  bool ok = true, any_pair = false;
+  for (int e = last_at_most(units, n_entries, begin), last = last_at_most(units, n_entries, end - 1); e <= last; ++e)
+    any_pair = any_pair || (ctrl->pairs[e >> 5] >> (e & 31) & 1);
+  const KeyRing<D> keys = {!any_pair};
   if (warp == 8) {
-    // ------------------------------------------------------------ copies: K_0, K_1, V_0, K_2, V_1, ..
+    // ------------------------------------------------------------ copies of keys
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kServiceRegs));
-    int nk = 0, nv = 0;                                    // tiles of keys and of values requested so far
+    int nk = 0;                                            // tiles requested so far
     for (int at = begin; at < end && ok;) {
       const Piece k = piece_at(p, units, n_entries, at, end);
       at += k.units;
       if (k.n == 0) continue;
-      const bool own = k.e >= p.n_groups;
       const Source src = source_of(p, k);
-      int next = box_row(p, src, k.tile0), before = -1;
-      for (int j = 0; j <= k.n && ok; ++j) {
-        const int row = next;
+      int next = box_row(p, src, k.tile0);                 // (looked up a tile ahead)
+      for (int j = 0; j < k.n; ++j, ++nk) {
+        const int row = next, st = keys.stage(nk);
         if (j + 1 < k.n) next = box_row(p, src, k.tile0 + j + 1);
-        if (j < k.n) {
-          const int st = nk % kDepth;
-          ok = __all_sync(0xffffffffu, mbar_wait(&k_empty[st], ((nk / kDepth) & 1) ^ 1, abort_flag));
-          if (!ok) break;
-          copy_tile<D>(src, own ? tmap_k : tmap_kx, smem + L::kKeys + st * L::kTileBytes, &k_full[st], k.head, row);
-          ++nk;
-        }
-        if (j > 0) {
-          const int st = nv % kDepth;
-          ok = __all_sync(0xffffffffu, mbar_wait(&v_empty[st], ((nv / kDepth) & 1) ^ 1, abort_flag));
-          if (!ok) break;
-          copy_tile<D>(src, own ? tmap_v : tmap_vx, smem + L::kValues + st * L::kTileBytes, &v_full[st], k.head, before);
-          ++nv;
-        }
-        before = row;
+        ok = __all_sync(0xffffffffu, mbar_wait(&k_empty[st], keys.phase(nk) ^ 1, abort_flag));
+        if (!ok) break;
+        copy_tile<D>(src, k.e >= p.n_groups ? tmap_k : tmap_kx, smem + KeyRing<D>::offset(st), &k_full[st], k.head, row);
       }
     }
     if (!ok) {
       // leave no copy in flight: wait (bounded) for the tiles already requested
-      for (int i = max(0, nk - kDepth); i < nk; ++i)
+      for (int i = max(0, nk - keys.depth()); i < nk; ++i)
         for (uint32_t spin = 0; spin < (1u << 20); ++spin)
-          if (mbar_try_wait(&k_full[i % kDepth], (i / kDepth) & 1)) break;
-      for (int i = max(0, nv - kDepth); i < nv; ++i)
-        for (uint32_t spin = 0; spin < (1u << 20); ++spin)
-          if (mbar_try_wait(&v_full[i % kDepth], (i / kDepth) & 1)) break;
+          if (mbar_try_wait(&k_full[keys.stage(i)], keys.phase(i))) break;
     }
   } else if (warp == 9) {
     // ------------------------------------------------------------ products
@@ -550,7 +602,6 @@ __device__ __forceinline__ void many_rows(const SharedParams &p, const CUtensorM
     if (elect_one()) {
       constexpr uint32_t idesc_qk = make_idesc_bf16(128, kTile, 0), idesc_pv = make_idesc_bf16(128, D, 1);
       const uint64_t q_desc = make_smem_desc(smem_u32(smem), 16, 1024);
-      const uint64_t k_desc = make_smem_desc(smem_u32(smem + L::kKeys), 16, 1024);
       const uint64_t v_desc = make_smem_desc(smem_u32(smem + L::kValues), L::kRegion, 1024);
       int nk = 0, nv = 0, n_pieces = 0;                    // tiles of all earlier pieces; pieces
       int p_uses[2] = {0, 0}, o_uses[2] = {0, 0};
@@ -560,18 +611,19 @@ __device__ __forceinline__ void many_rows(const SharedParams &p, const CUtensorM
         if (k.n == 0) continue;
         const bool pair = k.n_rows > 128;
         const int n = k.n, step = pair ? 1 : 2;
-        auto wait_k = [&](int j) { return mbar_wait(&k_full[(nk + j) % kDepth], ((nk + j) / kDepth) & 1, abort_flag); };
+        auto wait_k = [&](int j) { return mbar_wait(&k_full[keys.stage(nk + j)], keys.phase(nk + j), abort_flag); };
         auto wait_v = [&](int j) { return mbar_wait(&v_full[(nv + j) % kDepth], ((nv + j) / kDepth) & 1, abort_flag); };
         auto issue_qk = [&](int t, int j) {
           const uint64_t qd = q_desc + (uint64_t)((pair && t ? L::kTileBytes : 0) >> 4);
-          const uint64_t kd = k_desc + (uint64_t)((((nk + j) % kDepth) * L::kTileBytes) >> 4);
+          const int st = keys.stage(nk + j);
+          const uint64_t kd = q_desc + (uint64_t)(KeyRing<D>::offset(st) >> 4);
 #pragma unroll
           for (int c = 0; c < D / 16; ++c) {
             const uint64_t off = (uint64_t)(((c >> 2) * L::kRegion + (c & 3) * 32) >> 4);
             mma_ss(tmem + t * 128, qd + off, kd + off, idesc_qk, c > 0);
           }
           mma_commit(&ctrl->s_full[t]);
-          if (!pair || t) mma_commit(&k_empty[(nk + j) % kDepth]);
+          if (!pair || t) mma_commit(&k_empty[st]);
           if (j + 1 == n && (!pair || t)) mma_commit(&ctrl->q_empty);         // that was the piece's last product with the queries
         };
         auto issue_pv = [&](int t, int j, bool first, int half) {
@@ -586,7 +638,7 @@ __device__ __forceinline__ void many_rows(const SharedParams &p, const CUtensorM
         for (int t = 0; t < 2; ++t) {
           const int j = pair ? 0 : t;
           if (!ok || j >= n) continue;
-          ok = wait_k(j);
+          if (!pair || t == 0) ok = wait_k(j);
           if (!ok) continue;
           tc_fence_after();
           issue_qk(t, j);
@@ -597,14 +649,14 @@ __device__ __forceinline__ void many_rows(const SharedParams &p, const CUtensorM
             const int j = pair ? i : 2 * i + t, jn = j + step;
             if (!ok || j >= n) continue;
             const bool last = jn >= n;
-            ok = wait_v(j);
+            if (!pair || t == 0) ok = wait_v(j);           // (a wait costs this thread some 220 cycles: none twice)
             // the first product of a piece overwrites O_t: the rows before it must have been read out
             if (ok && i == 0) ok = mbar_wait(&ctrl->o_free[t], (o_uses[t] & 1) ^ 1, abort_flag);
             if (ok) ok = mbar_wait(&ctrl->p_full[t][0], p_uses[t] & 1, abort_flag);
             if (!ok) continue;
             tc_fence_after();
             issue_pv(t, j, i == 0, 0);
-            if (!last) ok = wait_k(jn);                    // (needed right after; off the critical path here)
+            if (!last && (!pair || t == 0)) ok = wait_k(jn);                   // (needed right after; off the critical path here)
             if (ok) ok = mbar_wait(&ctrl->p_full[t][1], p_uses[t] & 1, abort_flag);
             if (!ok) continue;
             tc_fence_after();
@@ -619,28 +671,62 @@ __device__ __forceinline__ void many_rows(const SharedParams &p, const CUtensorM
       }
     }
   } else if (warp >= 10) {
-    // ------------------------------------------------------------ queries: 16 bytes a copy, into the tiles' swizzled layout
+    // ------------------------------------------------------------ warp 10: copies of values; warp 11, and both for the first piece: queries
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kServiceRegs));
-    int n_pieces = 0;
+    const bool values = warp == 10;
+    int nv = 0, n_pieces = 0, n_q = 0;                     // tiles and pieces so far; of those, with queries fetched by the copy engine
     for (int at = begin; at < end && ok;) {
       const Piece k = piece_at(p, units, n_entries, at, end);
       at += k.units;
       if (k.n == 0) continue;
-      ok = mbar_wait(&ctrl->q_empty, (n_pieces & 1) ^ 1, abort_flag);
+      if (!values) ok = __all_sync(0xffffffffu, mbar_wait(&ctrl->q_empty, (n_pieces & 1) ^ 1, abort_flag));
       if (!ok) break;
-      ++n_pieces;
-      constexpr int kVecs = D / 8;
-      const int tile_rows = k.n_rows > 128 ? 256 : 128, c = (threadIdx.x - 320) % kVecs;
-      const RowMap map(p, k.x, k.row0, k.head);
-      const uint32_t base = smem_u32(smem) + (c >> 3) * L::kRegion;
+      const int tile_rows = k.n_rows > 128 ? 256 : 128;
+      if (p.q_boxes) {                                     // the heads of a group divide a tile: boxes of whole tokens
+        if (!values && lane == 0) {
+          mbar_arrive_expect_tx(&ctrl->q_full, tile_rows * D * 2);
+          for (int t = 0; t * 128 < tile_rows; ++t)
+            for (int c = 0; c < D / 64; ++c)
+              tma_load_3d(smem + t * L::kTileBytes + c * L::kRegion, tmap_q, &ctrl->q_full, c * 64, k.head * p.G, k.x.q_row0 + (k.row0 + t * 128) / p.G);
+        }
+        __syncwarp();
+        n_q = n_pieces + 1;
+      } else if (!values || n_pieces == 0) {               // 16 bytes a copy, into the tiles' swizzled layout
+        constexpr int kVecs = D / 8;
+        const int thread = n_pieces == 0 ? (int)threadIdx.x - 320 : lane, threads = n_pieces == 0 ? 64 : 32;
+        const int c = thread % kVecs;
+        const RowMap map(p, k.x, k.row0, k.head);
+        const uint32_t base = smem_u32(smem) + (c >> 3) * L::kRegion;
 #pragma unroll 8
-      for (int r = (threadIdx.x - 320) / kVecs; r < tile_rows; r += 64 / kVecs) {
-        const bool there = r < k.n_rows;                   // (rows that are not there are zeros: they take part in no maximum)
-        copy_16_or_zero(base + (r >> 7) * L::kTileBytes + (r & 127) * 128 + (((c & 7) ^ (r & 7)) << 4), p.q + map.row(there ? r : 0) * D + c * 8, there);
+        for (int r = thread / kVecs; r < tile_rows; r += threads / kVecs) {
+          const bool there = r < k.n_rows;                 // (rows that are not there are zeros)
+          copy_16_or_zero(base + (r >> 7) * L::kTileBytes + (r & 127) * 128 + (((c & 7) ^ (r & 7)) << 4), p.q + map.row(there ? r : 0) * D + c * 8, there);
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        fence_proxy_async();                               // the tensor core reads through the async proxy
+        if (n_pieces == 0) asm volatile("bar.sync 2, 64;" ::: "memory");       // (no wait of either warp before it can expire)
+        else __syncwarp();
+        if (!values && lane == 0) mbar_arrive(&ctrl->q_full);
       }
-      asm volatile("cp.async.wait_all;" ::: "memory");
-      fence_proxy_async();                                 // the tensor core reads through the async proxy
-      mbar_arrive(&ctrl->q_full);
+      ++n_pieces;
+      if (!values) continue;
+      const Source src = source_of(p, k);
+      int next = box_row(p, src, k.tile0);
+      for (int j = 0; j < k.n; ++j, ++nv) {
+        const int row = next, st = nv % kDepth;
+        if (j + 1 < k.n) next = box_row(p, src, k.tile0 + j + 1);
+        ok = __all_sync(0xffffffffu, mbar_wait(&v_empty[st], ((nv / kDepth) & 1) ^ 1, abort_flag));
+        if (!ok) break;
+        copy_tile<D>(src, k.e >= p.n_groups ? tmap_v : tmap_vx, smem + L::kValues + st * L::kTileBytes, &v_full[st], k.head, row);
+      }
+    }
+    if (!ok && !values && n_q > 0)                         // leave no copy in flight: wait (bounded) for what was requested
+      for (uint32_t spin = 0; spin < (1u << 20); ++spin)
+        if (mbar_try_wait(&ctrl->q_full, (n_q - 1) & 1)) break;
+    if (!ok && values) {
+      for (int i = max(0, nv - kDepth); i < nv; ++i)
+        for (uint32_t spin = 0; spin < (1u << 20); ++spin)
+          if (mbar_try_wait(&v_full[i % kDepth], (i / kDepth) & 1)) break;
     }
   } else {
     // ------------------------------------------------------------ softmax, a thread a row
@@ -686,7 +772,8 @@ __device__ __forceinline__ void many_rows(const SharedParams &p, const CUtensorM
         if (j == j0) {
           m_used = m_new;
         } else {
-          const bool grow = (m_new - m_used) * sl > kRescale;                  // (from -inf: yes)
+          // (from -inf: yes; rows that are not the item's have no say, so that results do not depend on what lies there)
+          const bool grow = row < k.n_rows && (m_new - m_used) * sl > kRescale;
           if (__any_sync(0xffffffffu, grow)) {
             // 1 when this row's maximum did not move (also when the row has seen no key yet)
             const float alpha = (m_new == -INFINITY) ? 1.f : ex2((m_used - m_new) * sl);
@@ -799,7 +886,7 @@ template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
 ba_shared_attend_kernel(const __grid_constant__ CUtensorMap tmap_kx, const __grid_constant__ CUtensorMap tmap_vx,
                         const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
-                        const __grid_constant__ SharedParams p) {
+                        const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ SharedParams p) {
   using L = SharedLayout<D>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -810,8 +897,9 @@ ba_shared_attend_kernel(const __grid_constant__ CUtensorMap tmap_kx, const __gri
   const int n_entries = p.n_groups + p.batch, n_ctas = (int)gridDim.x;
   if (tid == 0) {
     for (int i = 0; i < L::kStages; ++i) { mbar_init(&ctrl->full[i], 1); mbar_init(&ctrl->empty[i], kWarps); }
-    for (int i = 0; i < L::kDepth; ++i) { mbar_init(&ctrl->k_full[i], 1); mbar_init(&ctrl->k_empty[i], 1); mbar_init(&ctrl->v_full[i], 1); mbar_init(&ctrl->v_empty[i], 1); }
-    mbar_init(&ctrl->q_full, 64); mbar_init(&ctrl->q_empty, 1);
+    for (int i = 0; i <= L::kDepth; ++i) { mbar_init(&ctrl->k_full[i], 1); mbar_init(&ctrl->k_empty[i], 1); }
+    for (int i = 0; i < L::kDepth; ++i) { mbar_init(&ctrl->v_full[i], 1); mbar_init(&ctrl->v_empty[i], 1); }
+    mbar_init(&ctrl->q_full, 1); mbar_init(&ctrl->q_empty, 1);
     for (int t = 0; t < 2; ++t) {
       mbar_init(&ctrl->s_full[t], 1); mbar_init(&ctrl->p_full[t][0], 128); mbar_init(&ctrl->p_full[t][1], 128);
       mbar_init(&ctrl->o_done[t], 1); mbar_init(&ctrl->o_free[t], 128);
@@ -819,9 +907,9 @@ ba_shared_attend_kernel(const __grid_constant__ CUtensorMap tmap_kx, const __gri
     ctrl->abort_flag = 0; ctrl->invalid = 0;
     fence_barrier_init();
   }
-  if (tid >= 32 && tid < 32 + kMaxEntries / 32) ctrl->alone[tid - 32] = 0;
+  if (tid >= 32 && tid < 32 + kMaxEntries / 32) { ctrl->alone[tid - 32] = 0; ctrl->pairs[tid - 32] = 0; }
   if (warp == 9) { tmem_alloc(&ctrl->tmem_base, 512); tmem_relinquish(); }
-  if (warp == kWarps && elect_one()) { prefetch_tmap(&tmap_k); prefetch_tmap(&tmap_v); prefetch_tmap(&tmap_kx); prefetch_tmap(&tmap_vx); }
+  if (warp == kWarps && elect_one()) { prefetch_tmap(&tmap_k); prefetch_tmap(&tmap_v); prefetch_tmap(&tmap_kx); prefetch_tmap(&tmap_vx); prefetch_tmap(&tmap_q); }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -829,67 +917,68 @@ ba_shared_attend_kernel(const __grid_constant__ CUtensorMap tmap_kx, const __gri
   ba_pdl_trigger();
   // The streams: units before every entry, by kind, and what the entries of many rows cost.  A thread takes neighbouring entries.
   const int per = (n_entries + kThreads - 1) / kThreads, e0 = min(n_entries, tid * per), e1 = min(n_entries, e0 + per);
-  double sum[2] = {0, 0}, cost = 0;
+  int sum[2] = {0, 0};
   Entry one;                                               // (a thread's only entry, where there are no more than threads)
   for (int e = e0; e < e1; ++e) {
-    if (!load_entry(p, e, one)) { ctrl->invalid = 1; one.len = one.rows = 0; }
-    const double n = (double)row_tiles_of(p, one) * p.Hkv * item_units(p, one);
-    sum[is_many(p, one)] += n;
-    if (is_many(p, one)) {
-      const int left = one.rows * p.G % kManyRows;         // (rows of the last item, if it is not full)
-      cost += n * kCostPair - (left > 0 && left <= 128 ? (double)p.Hkv * item_units(p, one) * (kCostPair - kCostSolo) : 0.);
-    }
+    bool good = load_entry(p, e, one);
+    const long long n = lay_of(p, one).a_head() * p.Hkv;
+    good = good && sum[0] + sum[1] + n <= kMostUnits;
+    if (!good) { ctrl->invalid = 1; break; }
+    sum[is_many(p, one)] += (int)n;
+    if (one.rows * p.G > 128) atomicOr(&ctrl->pairs[e >> 5], 1u << (e & 31));
     if (e >= p.n_groups) {
       const int g = group_of(p, e - p.n_groups);
       if (g < 0 || __ldg(p.prefix_cu + g + 1) == __ldg(p.prefix_cu + g)) atomicOr(&ctrl->alone[e >> 5], 1u << (e & 31));
     }
   }
-  // (sums in doubles, whole numbers up to 2^53, so that what is too much shows)
-  const double mine[2] = {sum[0], sum[1]};
+  const int mine[2] = {sum[0], sum[1]};
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
-    const double a = __shfl_up_sync(0xffffffffu, sum[0], d), b = __shfl_up_sync(0xffffffffu, sum[1], d), c = __shfl_up_sync(0xffffffffu, cost, d);
-    if (lane >= d) { sum[0] += a; sum[1] += b; cost += c; }
+    const int a = __shfl_up_sync(0xffffffffu, sum[0], d), b = __shfl_up_sync(0xffffffffu, sum[1], d);
+    if (lane >= d) { sum[0] += a; sum[1] += b; }
   }
-  if (lane == 31) {
-    ctrl->warp_units[0][warp] = sum[0]; ctrl->warp_units[1][warp] = sum[1]; ctrl->warp_cost[warp] = cost;
-  }
+  if (lane == 31) ctrl->warp_sums[warp] = make_int2(sum[0], sum[1]);
   __syncthreads();
-  double total[2] = {0, 0}, cost_many = 0;
+  int total[2] = {0, 0};
+#pragma unroll
   for (int w = 0; w < kThreads / 32; ++w) {
-    if (w == warp) { sum[0] += total[0]; sum[1] += total[1]; }
-    total[0] += ctrl->warp_units[0][w]; total[1] += ctrl->warp_units[1][w]; cost_many += ctrl->warp_cost[w];
+    const int2 v = ctrl->warp_sums[w];
+    if (w < warp) { sum[0] += v.x; sum[1] += v.y; }
+    total[0] += v.x; total[1] += v.y;
   }
-  const bool valid = !ctrl->invalid && total[0] < 2e9 && total[1] < 2e9;
+  const bool valid = !ctrl->invalid;
   // CTAs for many rows
   int n_many = 0;
-  if (total[1] > 0) {
-    n_many = (int)((double)n_ctas * cost_many / (cost_many + total[0] * kCostFew) + 0.5);
+  if (valid && total[1] > 0) {
+    const float few = (float)total[0] * kCostFew, more = (float)total[1] * kCostMany;
+    n_many = (int)((float)n_ctas * more / (more + few) + 0.5f);
     n_many = max(1, min(n_many, total[0] > 0 ? n_ctas - 1 : n_ctas));
   }
   const int n_few = n_ctas - n_many;
-  const int run[2] = {valid && n_few ? ((int)total[0] + n_few - 1) / n_few : 0, valid && n_many ? ((int)total[1] + n_many - 1) / n_many : 0};
+  // (a run is a tile at least: every CTA between an item's first and last tile has one of it)
+  const int run[2] = {valid && n_few ? max(kTileFew, (int)(((unsigned)total[0] + n_few - 1) / n_few)) : 0,
+                      valid && n_many ? max(kTilePair, (int)(((unsigned)total[1] + n_many - 1) / n_many)) : 0};
   if (valid) {
-    int u[2] = {(int)(sum[0] - mine[0]), (int)(sum[1] - mine[1])};
+    int u[2] = {sum[0] - mine[0], sum[1] - mine[1]};
     for (int e = e0; e < e1; ++e) {
       units[e] = u[0]; units_many[e] = u[1];
       const Entry x = per == 1 ? one : get_entry(p, e);
       const bool many = is_many(p, x);
       if (blockIdx.x == 0) p.meta[e] = make_int4(u[many], tiles_of(x), x.rows * p.G, many);
-      u[many] += row_tiles_of(p, x) * p.Hkv * item_units(p, x);
+      u[many] += (int)lay_of(p, x).a_head() * p.Hkv;
     }
-    if (tid == kThreads - 1) { units[n_entries] = (int)total[0]; units_many[n_entries] = (int)total[1]; }
+    if (tid == kThreads - 1) { units[n_entries] = total[0]; units_many[n_entries] = total[1]; }
   }
   if (blockIdx.x == 0 && tid == 0) {
     p.meta[n_entries] = make_int4(run[0], run[1], n_many, valid);
     if (!valid) ba_record_status(p.status, BA_ERR_INVALID_ARG);
   }
   const bool many = (int)blockIdx.x < n_many;
-  const int nth = many ? (int)blockIdx.x : (int)blockIdx.x - n_many, all = valid ? (int)total[many] : 0;
+  const int nth = many ? (int)blockIdx.x : (int)blockIdx.x - n_many, all = valid ? total[many] : 0;
   const int begin = (int)min((long long)all, (long long)run[many] * nth), end = min(all, begin + run[many]);
   __syncthreads();
   if (begin < end) {
-    if (many) many_rows<D>(p, &tmap_kx, &tmap_vx, &tmap_k, &tmap_v, smem, ctrl, units_many, n_entries, begin, end);
+    if (many) many_rows<D>(p, &tmap_kx, &tmap_vx, &tmap_k, &tmap_v, &tmap_q, smem, ctrl, units_many, n_entries, begin, end);
     else few_rows<D>(p, &tmap_kx, &tmap_vx, &tmap_k, &tmap_v, smem, ctrl, units, n_entries, begin, end);
   }
   tc_fence_before();
@@ -902,53 +991,74 @@ ba_shared_attend_kernel(const __grid_constant__ CUtensorMap tmap_kx, const __gri
 // row of an output head; what it waits for is looked up side by side.
 template <int D>
 __global__ void __launch_bounds__(256)
-ba_shared_merge_kernel(const __grid_constant__ SharedParams p) {
+ba_shared_merge_kernel(const __grid_constant__ SharedParams p, int warps_a_row) {
   constexpr int kV = D / 32;                               // columns of a lane
-  const int lane = threadIdx.x & 31;
-  const long long u = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
-  ba_pdl_wait();
-  ba_pdl_trigger();
-  const int4 head = p.meta[p.n_groups + p.batch];          // (plain loads: the kernel before wrote them)
-  if (!head.w || u >= (long long)p.n_q_rows * p.Hq) return;
-  const int row = (int)(u / p.Hq), hq = (int)(u - (long long)row * p.Hq), h = hq / p.G;
-  int s = row;
-  if (p.q_cu) {
+  __shared__ float others[8][32 * kV + 2];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int share = warp & (warps_a_row - 1);              // this warp's share of the row's results
+  const long long u = ((long long)blockIdx.x * 8 + warp) / warps_a_row;
+  // Whose row this is, while the kernel before is still at work: the caller's tables are not that kernel's, and what wrote them had
+  // completed when it let this one start.
+  const bool there = u < (long long)p.n_q_rows * p.Hq;
+  const int row = there ? (int)(u / p.Hq) : 0, hq = there ? (int)(u - (long long)row * p.Hq) : 0, h = hq / p.G;
+  int s = row, g = -1, row0[2] = {0, 0};
+  if (there && p.q_cu) {
     int lo = 0, hi = p.batch + 1;
     while (lo < hi) { const int mid = (lo + hi) >> 1; if (__ldg(p.q_cu + mid) <= row) lo = mid + 1; else hi = mid; }
     s = lo - 1;
   }
-  if (s < 0 || s >= p.batch) return;
-  const int g = group_of(p, s);
+  // (a warp whose row is not there or complete goes on without results: the warps of a CTA meet)
+  bool needed = there && s >= 0 && s < p.batch;
+  if (needed) {
+    g = group_of(p, s);
+    row0[1] = q_begin(p, s);
+    if (g >= 0 && p.group_cu) { const int a = __ldg(p.group_cu + g); row0[0] = a >= 0 && a <= p.batch ? q_begin(p, a) : 0; }    // (not checked yet)
+    else if (g >= 0) row0[0] = q_begin(p, 0);
+  }
+  ba_pdl_wait();
+  ba_pdl_trigger();
+  const int4 head = p.meta[p.n_groups + p.batch];          // (plain loads: the kernel before wrote them)
+  needed = needed && head.w;
   // results of this row: first pieces, then those of CTAs, of its prefix (0) and of its own rows (1)
-  int n[2] = {0, 0}, c0[2], per[2], tile_row[2];
+  int n[2] = {0, 0}, c0[2] = {0, 0}, per[2] = {1, 1}, tile_row[2] = {0, 0};
+  if (needed) {
 #pragma unroll
-  for (int side = 0; side < 2; ++side) {
-    if (side == 0 && g < 0) continue;
-    const int e = side == 0 ? g : p.n_groups + s;
-    const int4 m = p.meta[e];
-    if (m.y == 0) continue;
-    const int row0 = side == 0 ? q_begin(p, p.group_cu ? __ldg(p.group_cu + g) : 0) : q_begin(p, s);
-    const int r = (row - row0) * p.G + hq - h * p.G, front = m.w ? kItemMany : kItemFew, all = m.y + front;
-    const int rts = m.w ? (m.z + kManyRows - 1) / kManyRows : 1, rt = m.w ? r / kManyRows : 0, run = m.w ? head.y : head.x;
-    const int a = m.x + (h * rts + rt) * all;
-    c0[side] = (a + front) / run;
-    const int pieces = (a + all - 1) / run - c0[side] + 1;
-    if (side == 1 && n[0] == 0 && pieces == 1 && !m.w) return;                 // whole, and nothing beside it: written where it was computed
-    c0[side] += m.w ? 0 : head.z;
-    per[side] = m.w && m.z - rt * kManyRows <= 128 ? 2 : 1;                    // each softmax group left a result
-    n[side] = pieces * per[side];
-    tile_row[side] = r - rt * kManyRows;
+    for (int side = 0; side < 2; ++side) {
+      if (side == 0 && g < 0) continue;
+      const int e = side == 0 ? g : p.n_groups + s;
+      const int4 m = p.meta[e];
+      if (m.y == 0) continue;
+      const int r = (row - row0[side]) * p.G + hq - h * p.G, rt = m.w ? r / kManyRows : 0, run = m.w ? head.y : head.x;
+      const Lay lay(m.y, m.z, m.w != 0);
+      const int first_tile = m.x + h * (int)lay.a_head() + rt * lay.full + lay.front;
+      const int w = tile_units(m.w != 0, m.z - rt * kManyRows);
+      c0[side] = first_tile / run;
+      const int pieces = (first_tile + (m.y - 1) * w) / run - c0[side] + 1;
+      if (side == 1 && n[0] == 0 && pieces == 1 && !m.w) { needed = false; continue; }       // whole, and nothing beside it: written where it was computed
+      c0[side] += m.w ? 0 : head.z;
+      per[side] = m.w && m.z - rt * kManyRows <= 128 ? 2 : 1;                  // each softmax group left a result
+      n[side] = pieces * per[side];
+      tile_row[side] = r - rt * kManyRows;
+    }
   }
   const long long here = (long long)row * p.Hq + hq;
+  const int total = n[0] + n[1], i_end = (share + 1) * total / warps_a_row;
   float top = -INFINITY, den = 0.f, acc[kV];
 #pragma unroll
   for (int v = 0; v < kV; ++v) acc[v] = 0.f;
+  auto rescale = [&](float mx) {
+    const float f = __expf(top - mx);                      // (0 from -infinity)
+    top = mx;
+    den *= f;
+#pragma unroll
+    for (int v = 0; v < kV; ++v) acc[v] *= f;
+  };
   // a lane looks up one result of 32; what is not empty is added, the values of several on their way at a time
-  for (int i0 = 0; i0 < n[0] + n[1]; i0 += 32) {
+  for (int i0 = share * total / warps_a_row; i0 < i_end; i0 += 32) {
     const int i = i0 + lane;
     long long at = 0;
     float lse = -INFINITY;
-    if (i < n[0] + n[1]) {
+    if (i < i_end) {
       const int side = i >= n[0], k = i - (side ? n[0] : 0), pc = side ? per[1] : per[0], piece = k / pc, second = k - piece * pc;
       at = piece == 0 ? first_part(p, (side ? 0 : 1) + 2 * second) + here
                       : cut_part(p, (side ? c0[1] : c0[0]) + piece) + (side ? tile_row[1] : tile_row[0]) + 128 * second;
@@ -958,28 +1068,52 @@ ba_shared_merge_kernel(const __grid_constant__ SharedParams p) {
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
     if (mx == -INFINITY) continue;
-    const float before = __expf(top - mx), w = __expf(lse - mx);               // (0 from -infinity)
-    top = mx;
-    den *= before;
+    const float w = __expf(lse - mx);
+    rescale(mx);
+    const int count = min(32, i_end - i0);
+    for (int k0 = 0; k0 < count; k0 += 4) {
+      float wk[4], f[4][kV];
 #pragma unroll
-    for (int v = 0; v < kV; ++v) acc[v] *= before;
-    const int count = min(32, n[0] + n[1] - i0);
-#pragma unroll 8
-    for (int k = 0; k < count; ++k) {
-      const float wk = __shfl_sync(0xffffffffu, w, k);
-      const long long ak = __shfl_sync(0xffffffffu, at, k);
-      if (wk == 0.f) continue;                             // (an empty one holds no values at all)
-      const float *x = p.part + ak * D + lane * kV;
-      den += wk;
-      if (kV == 4) {
-        const float4 f = __ldcs(reinterpret_cast<const float4 *>(x));
-        acc[0] = fmaf(wk, f.x, acc[0]); acc[1] = fmaf(wk, f.y, acc[1]); acc[2 % kV] = fmaf(wk, f.z, acc[2 % kV]); acc[3 % kV] = fmaf(wk, f.w, acc[3 % kV]);
-      } else {
-        const float2 f = __ldcs(reinterpret_cast<const float2 *>(x));
-        acc[0] = fmaf(wk, f.x, acc[0]); acc[1] = fmaf(wk, f.y, acc[1]);
+      for (int k = 0; k < 4; ++k) {
+        wk[k] = __shfl_sync(0xffffffffu, w, (k0 + k) & 31);
+        const long long ak = __shfl_sync(0xffffffffu, at, (k0 + k) & 31);
+        if (k0 + k >= count) wk[k] = 0.f;
+        const float *x = p.part + ak * D + lane * kV;      // (an empty one holds no values at all)
+        if (kV == 4) {
+          const float4 v = wk[k] == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : __ldcs(reinterpret_cast<const float4 *>(x));
+          f[k][0] = v.x; f[k][1] = v.y; f[k][2 % kV] = v.z; f[k][3 % kV] = v.w;
+        } else {
+          const float2 v = wk[k] == 0.f ? make_float2(0.f, 0.f) : __ldcs(reinterpret_cast<const float2 *>(x));
+          f[k][0] = v.x; f[k][1] = v.y;
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        den += wk[k];
+#pragma unroll
+        for (int v = 0; v < kV; ++v) acc[v] = fmaf(wk[k], f[k][v], acc[v]);
       }
     }
   }
+  if (warps_a_row > 1) {                                   // the row's first warp adds the others' shares, in order
+    if (share > 0) {
+#pragma unroll
+      for (int v = 0; v < kV; ++v) others[warp][lane * kV + v] = acc[v];
+      if (lane == 0) { others[warp][32 * kV] = top; others[warp][32 * kV + 1] = den; }
+    }
+    __syncthreads();
+    if (share > 0) return;
+    for (int k = 1; k < warps_a_row; ++k) {
+      const float t = others[warp + k][32 * kV], d = others[warp + k][32 * kV + 1], mx = fmaxf(top, t);
+      if (t == -INFINITY) continue;
+      rescale(mx);
+      const float f = __expf(t - mx);
+      den = fmaf(d, f, den);
+#pragma unroll
+      for (int v = 0; v < kV; ++v) acc[v] = fmaf(others[warp + k][lane * kV + v], f, acc[v]);
+    }
+  }
+  if (!needed) return;
   const float inv = den > 0.f ? 1.f / den : 0.f;
 #pragma unroll
   for (int v = 0; v < kV; ++v) acc[v] *= inv;
@@ -1069,11 +1203,13 @@ ba_status ba_shared_prefix_attend(ba_ctx *ctx, const void *q, int32_t n_q_rows, 
   p.meta = (int4 *)scratch;
   p.part = (float *)(scratch + meta_bytes(n_entries));
   p.n_part = n_part;
-  CUtensorMap tk, tv, tkx, tvx;
+  CUtensorMap tk, tv, tkx, tvx, tq;
   const long long rows = (long long)pages->n_pages * pages->page_rows;
   const int box = std::min(kTile, pages->page_rows);
   if (!ba_tensor_map(ctx, &tk, k_pool, p.Hkv, rows, 1, box) || !ba_tensor_map(ctx, &tv, v_pool, p.Hkv, rows, 1, box)) return BA_ERR_CUDA;
-  tkx = tk; tvx = tv;
+  tkx = tk; tvx = tv; tq = tk;
+  p.q_boxes = p.G <= 128 && 128 % p.G == 0;
+  if (p.q_boxes && !ba_tensor_map(ctx, &tq, q, p.Hq, n_q_rows, p.G, 128 / p.G)) return BA_ERR_CUDA;
   if (has_prefix) {
     const long long prows = prefix_pages ? (long long)prefix_pages->n_pages * prefix_pages->page_rows : n_prefix_rows;
     const int pbox = prefix_pages ? std::min(kTile, prefix_pages->page_rows) : kTile;
@@ -1081,13 +1217,16 @@ ba_status ba_shared_prefix_attend(ba_ctx *ctx, const void *q, int32_t n_q_rows, 
   }
   const dim3 grid((unsigned)ctx->sm_count);
   const cudaStream_t cs = (cudaStream_t)stream;
-  const unsigned merge = (unsigned)(((long long)n_q_rows * p.Hq + 7) / 8);
+  // Few rows with long prefixes have more results than a warp wants to wait for (16 requests over 32000 tokens: 35 a row, 512 rows):
+  // four warps a row while that leaves the GPU room.
+  const int warps_a_row = (long long)n_q_rows * p.Hq <= 4096 ? 4 : 1;
+  const unsigned merge = (unsigned)(((long long)n_q_rows * p.Hq * warps_a_row + 7) / 8);
   if (D == 128) {
-    BA_CUDA_TRY(ba_launch(ba_shared_attend_kernel<128>, grid, kThreads, SharedLayout<128>::kBytes, cs, true, tkx, tvx, tk, tv, p));
-    BA_CUDA_TRY(ba_launch(ba_shared_merge_kernel<128>, dim3(merge), 256, 0, cs, true, p));
+    BA_CUDA_TRY(ba_launch(ba_shared_attend_kernel<128>, grid, kThreads, SharedLayout<128>::kBytes, cs, true, tkx, tvx, tk, tv, tq, p));
+    BA_CUDA_TRY(ba_launch(ba_shared_merge_kernel<128>, dim3(merge), 256, 0, cs, true, p, warps_a_row));
   } else {
-    BA_CUDA_TRY(ba_launch(ba_shared_attend_kernel<64>, grid, kThreads, SharedLayout<64>::kBytes, cs, true, tkx, tvx, tk, tv, p));
-    BA_CUDA_TRY(ba_launch(ba_shared_merge_kernel<64>, dim3(merge), 256, 0, cs, true, p));
+    BA_CUDA_TRY(ba_launch(ba_shared_attend_kernel<64>, grid, kThreads, SharedLayout<64>::kBytes, cs, true, tkx, tvx, tk, tv, tq, p));
+    BA_CUDA_TRY(ba_launch(ba_shared_merge_kernel<64>, dim3(merge), 256, 0, cs, true, p, warps_a_row));
   }
   ctx->launches += 2;
   return BA_OK;
