@@ -442,7 +442,7 @@ ba_status ba_qk_norm_rope(ba_ctx *ctx, const void *q, int64_t q_stride, const vo
  *   dq, dk       rows `dq_stride`, `dk_stride` elements apart (0: packed; else a multiple of 16 bytes); may be dy_q, dy_k themselves where packed
  *   dw_q, dw_k   fp32 [head_dim], written (not added to); given exactly where w_q, w_k are.  Zero for n_rows = 0.
  *   grad_dtype   type of dy_q, dy_k, dq and dk
- * Uses 592 * 8 * head_dim bytes of workspace when there is a norm.  No atomics: results are run-to-run identical.
+ * Uses up to 592 * 8 * head_dim bytes of workspace when there is a norm (ba_workspace_bytes() counts them).  No atomics: results are run-to-run identical.
  */
 ba_status ba_qk_norm_rope_bwd(ba_ctx *ctx, const void *q, int64_t q_stride, const void *k, int64_t k_stride, int32_t n_rows,
                               const int32_t *pos, const void *w_q, const void *w_k, float eps, const void *dy_q, const void *dy_k,
@@ -490,10 +490,11 @@ typedef struct {
  *                from row prefix_cu[g] (the k_out of ba_final_attend_fused or the k_dst of ba_reencode_k, beside the cached values);
  *                else pools of that table, prefix g on list g (n_prefix_rows is not used)
  *   k_pool, v_pool, pages   the sequences' own rows, sequence s on list s (ba_append_paged fills them); may be the prefixes' pools
- *   o            [n_q_rows, n_q_heads, head_dim] bf16 or fp32; lse fp32 [n_q_rows, n_q_heads] or NULL
+ *   o            [n_q_rows, n_q_heads, head_dim] bf16 or fp32, apart from every input; lse fp32 [n_q_rows, n_q_heads] or NULL
  * What lies behind the end of a prefix, a sequence or a list in pages or rows is never used and may hold any bits.  A page number outside
  * its pool counts as zeros and is reported (BA_ERR_INVALID_ARG).  Tables that do not fit together (a cumulative table that decreases
- * or leaves its range, a length below zero or above its list's pages) are reported the same way and nothing is written.
+ * or leaves its range, a length below zero or above its list's pages) are reported the same way and nothing is written; so is an
+ * amount of work beyond any memory (key tiles of 128 x KV heads x 256 query rows of one entry above five million).
  * Uses ba_shared_prefix_bytes() bytes of workspace at most (to be given to ba_create(); BA_ERR_WORKSPACE otherwise); batch + n_groups is
  * at most BA_SHARED_MAX (BA_ERR_UNSUPPORTED).  No atomics: results are run-to-run identical.
  */

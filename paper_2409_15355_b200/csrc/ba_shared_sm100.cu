@@ -102,7 +102,7 @@ struct SharedCtrl {
   uint64_t q_full, q_empty, s_full[2], p_full[2][2], o_done[2], o_free[2];
   int abort_flag, invalid;
   uint32_t tmem_base;
-  uint32_t alone[kMaxEntries / 32];   // a bit an entry: own rows of a sequence without prefix
+  uint32_t prefixed[kMaxEntries / 32];         // a bit a sequence: it has a prefix
   uint32_t pairs[kMaxEntries / 32];   // a bit an entry: it has items of more than 128 rows
   int2 warp_sums[kThreads / 32];      // units of few rows, of many
 };
@@ -326,7 +326,7 @@ __device__ __forceinline__ void consume_run(const SharedParams &p, FewRun run, u
   if (more) load_queries<D>(p, k, qa, limit);
   while (more) {                         // (to the end even after a wait that expired: the warps meet at barriers)
     const bool own = k.e >= p.n_groups;
-    const bool direct = own && k.n == k.tiles && (ctrl->alone[k.e >> 5] >> (k.e & 31) & 1);
+    const bool direct = own && k.n == k.tiles && !(ctrl->prefixed[(k.e - p.n_groups) >> 5] >> ((k.e - p.n_groups) & 31) & 1);
     const int n_rows = k.n_rows;
     float o[D / 8][4], mx[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f};
 #pragma unroll
@@ -907,7 +907,7 @@ ba_shared_attend_kernel(const __grid_constant__ CUtensorMap tmap_kx, const __gri
     ctrl->abort_flag = 0; ctrl->invalid = 0;
     fence_barrier_init();
   }
-  if (tid >= 32 && tid < 32 + kMaxEntries / 32) { ctrl->alone[tid - 32] = 0; ctrl->pairs[tid - 32] = 0; }
+  if (tid >= 32 && tid < 32 + kMaxEntries / 32) { ctrl->prefixed[tid - 32] = 0; ctrl->pairs[tid - 32] = 0; }
   if (warp == 9) { tmem_alloc(&ctrl->tmem_base, 512); tmem_relinquish(); }
   if (warp == kWarps && elect_one()) { prefetch_tmap(&tmap_k); prefetch_tmap(&tmap_v); prefetch_tmap(&tmap_kx); prefetch_tmap(&tmap_vx); prefetch_tmap(&tmap_q); }
   tc_fence_before();
@@ -926,9 +926,12 @@ ba_shared_attend_kernel(const __grid_constant__ CUtensorMap tmap_kx, const __gri
     if (!good) { ctrl->invalid = 1; break; }
     sum[is_many(p, one)] += (int)n;
     if (one.rows * p.G > 128) atomicOr(&ctrl->pairs[e >> 5], 1u << (e & 31));
-    if (e >= p.n_groups) {
-      const int g = group_of(p, e - p.n_groups);
-      if (g < 0 || __ldg(p.prefix_cu + g + 1) == __ldg(p.prefix_cu + g)) atomicOr(&ctrl->alone[e >> 5], 1u << (e & 31));
+    if (e < p.n_groups && one.len > 0) {                   // its sequences do not write their rows straight to the output
+      const int a = p.group_cu ? __ldg(p.group_cu + e) : 0, b = p.group_cu ? __ldg(p.group_cu + e + 1) : p.batch;
+      for (int w = a >> 5; w <= (b - 1) >> 5 && a < b; ++w) {
+        const unsigned from = w == a >> 5 ? ~0u << (a & 31) : ~0u, to = w == (b - 1) >> 5 ? ~0u >> (31 - ((b - 1) & 31)) : ~0u;
+        atomicOr(&ctrl->prefixed[w], from & to);
+      }
     }
   }
   const int mine[2] = {sum[0], sum[1]};
@@ -956,8 +959,10 @@ ba_shared_attend_kernel(const __grid_constant__ CUtensorMap tmap_kx, const __gri
   }
   const int n_few = n_ctas - n_many;
   // (a run is a tile at least: every CTA between an item's first and last tile has one of it)
-  const int run[2] = {valid && n_few ? max(kTileFew, (int)(((unsigned)total[0] + n_few - 1) / n_few)) : 0,
-                      valid && n_many ? max(kTilePair, (int)(((unsigned)total[1] + n_many - 1) / n_many)) : 0};
+  auto run_of = [&](int kind) {
+    const unsigned n = (unsigned)(kind ? n_many : n_few);
+    return valid && n > 0 ? max(kind ? kTilePair : kTileFew, (int)(((unsigned)total[kind] + n - 1) / n)) : 0;
+  };
   if (valid) {
     int u[2] = {sum[0] - mine[0], sum[1] - mine[1]};
     for (int e = e0; e < e1; ++e) {
@@ -970,12 +975,13 @@ ba_shared_attend_kernel(const __grid_constant__ CUtensorMap tmap_kx, const __gri
     if (tid == kThreads - 1) { units[n_entries] = total[0]; units_many[n_entries] = total[1]; }
   }
   if (blockIdx.x == 0 && tid == 0) {
-    p.meta[n_entries] = make_int4(run[0], run[1], n_many, valid);
+    p.meta[n_entries] = make_int4(run_of(0), run_of(1), n_many, valid);
     if (!valid) ba_record_status(p.status, BA_ERR_INVALID_ARG);
   }
   const bool many = (int)blockIdx.x < n_many;
   const int nth = many ? (int)blockIdx.x : (int)blockIdx.x - n_many, all = valid ? total[many] : 0;
-  const int begin = (int)min((long long)all, (long long)run[many] * nth), end = min(all, begin + run[many]);
+  const int run = run_of(many);
+  const int begin = (int)min((long long)all, (long long)run * nth), end = min(all, begin + run);
   __syncthreads();
   if (begin < end) {
     if (many) many_rows<D>(p, &tmap_kx, &tmap_vx, &tmap_k, &tmap_v, &tmap_q, smem, ctrl, units_many, n_entries, begin, end);
@@ -987,27 +993,29 @@ ba_shared_attend_kernel(const __grid_constant__ CUtensorMap tmap_kx, const __gri
   if (warp == 9) tmem_dealloc(ctrl->tmem_base, 512);
 }
 
-// The partial results of every (row, head): those of its group's prefix and of its own rows, weighted by their denominators.  A warp has a
-// row of an output head; what it waits for is looked up side by side.
-template <int D>
+// The partial results of every (row, head): those of its group's prefix and of its own rows, weighted by their denominators.  What a row
+// waits for is a chain of look-ups, so rows go side by side: eight lanes a row (30720 rows: 34 us with a warp each), or, with few rows,
+// whose long prefixes leave many results, a warp or several.
+template <int D, int kL>
 __global__ void __launch_bounds__(256)
 ba_shared_merge_kernel(const __grid_constant__ SharedParams p, int warps_a_row) {
-  constexpr int kV = D / 32;                               // columns of a lane
-  __shared__ float others[8][32 * kV + 2];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int share = warp & (warps_a_row - 1);              // this warp's share of the row's results
-  const long long u = ((long long)blockIdx.x * 8 + warp) / warps_a_row;
+  constexpr int kVec = D / kL < 4 ? D / kL : 4, kChunks = D / (kL * kVec);     // a lane has kChunks x kVec columns
+  constexpr int kV = kVec * kChunks, kBatch = kL == 32 ? 4 : 2;                // results whose values are on their way at a time
+  __shared__ float others[kL == 32 ? 8 : 1][32 * kV + 2];
+  const int lane = threadIdx.x % kL, warp = threadIdx.x >> 5;
+  const int share = kL == 32 ? warp & (warps_a_row - 1) : 0;                   // this warp's share of the row's results
+  const long long u = ((long long)blockIdx.x * (256 / kL) + threadIdx.x / kL) / warps_a_row;
   // Whose row this is, while the kernel before is still at work: the caller's tables are not that kernel's, and what wrote them had
   // completed when it let this one start.
   const bool there = u < (long long)p.n_q_rows * p.Hq;
-  const int row = there ? (int)(u / p.Hq) : 0, hq = there ? (int)(u - (long long)row * p.Hq) : 0, h = hq / p.G;
+  const int row = there ? (int)u / p.Hq : 0, hq = there ? (int)u - row * p.Hq : 0, h = hq / p.G;
   int s = row, g = -1, row0[2] = {0, 0};
   if (there && p.q_cu) {
     int lo = 0, hi = p.batch + 1;
     while (lo < hi) { const int mid = (lo + hi) >> 1; if (__ldg(p.q_cu + mid) <= row) lo = mid + 1; else hi = mid; }
     s = lo - 1;
   }
-  // (a warp whose row is not there or complete goes on without results: the warps of a CTA meet)
+  // (lanes whose row is not there or complete go on without results: the warps of a CTA meet)
   bool needed = there && s >= 0 && s < p.batch;
   if (needed) {
     g = group_of(p, s);
@@ -1042,60 +1050,61 @@ ba_shared_merge_kernel(const __grid_constant__ SharedParams p, int warps_a_row) 
     }
   }
   const long long here = (long long)row * p.Hq + hq;
-  const int total = n[0] + n[1], i_end = (share + 1) * total / warps_a_row;
+  const int total = n[0] + n[1], i_begin = share * total / warps_a_row, i_end = (share + 1) * total / warps_a_row;
   float top = -INFINITY, den = 0.f, acc[kV];
 #pragma unroll
   for (int v = 0; v < kV; ++v) acc[v] = 0.f;
+  // everything so far and `mx`, which may be -infinity like `top`, on a common scale
   auto rescale = [&](float mx) {
-    const float f = __expf(top - mx);                      // (0 from -infinity)
+    const float f = top == -INFINITY ? 0.f : __expf(top - mx);
     top = mx;
     den *= f;
 #pragma unroll
     for (int v = 0; v < kV; ++v) acc[v] *= f;
   };
-  // a lane looks up one result of 32; what is not empty is added, the values of several on their way at a time
-  for (int i0 = share * total / warps_a_row; i0 < i_end; i0 += 32) {
-    const int i = i0 + lane;
+  // A lane looks up one result of kL; what is not empty is added.  (The rows of a warp take as many rounds as its longest.)
+  const int rounds = __reduce_max_sync(0xffffffffu, i_end - i_begin);
+  for (int i0 = 0; i0 < rounds; i0 += kL) {
+    const int i = i_begin + i0 + lane;
     long long at = 0;
     float lse = -INFINITY;
     if (i < i_end) {
-      const int side = i >= n[0], k = i - (side ? n[0] : 0), pc = side ? per[1] : per[0], piece = k / pc, second = k - piece * pc;
+      const int side = i >= n[0], k = i - (side ? n[0] : 0), two = (side ? per[1] : per[0]) - 1, piece = k >> two, second = k & two;
       at = piece == 0 ? first_part(p, (side ? 0 : 1) + 2 * second) + here
                       : cut_part(p, (side ? c0[1] : c0[0]) + piece) + (side ? tile_row[1] : tile_row[0]) + 128 * second;
       lse = p.part[p.n_part * D + at];
     }
     float mx = fmaxf(lse, top);
 #pragma unroll
-    for (int d = 16; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
-    if (mx == -INFINITY) continue;
-    const float w = __expf(lse - mx);
+    for (int d = kL / 2; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+    const float w = lse == -INFINITY ? 0.f : __expf(lse - mx);
     rescale(mx);
-    const int count = min(32, i_end - i0);
-    for (int k0 = 0; k0 < count; k0 += 4) {
-      float wk[4], f[4][kV];
+    for (int k0 = 0; k0 < min(kL, rounds - i0); k0 += kBatch) {
+      float wk[kBatch], f[kBatch][kV];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        wk[k] = __shfl_sync(0xffffffffu, w, (k0 + k) & 31);
-        const long long ak = __shfl_sync(0xffffffffu, at, (k0 + k) & 31);
-        if (k0 + k >= count) wk[k] = 0.f;
-        const float *x = p.part + ak * D + lane * kV;      // (an empty one holds no values at all)
-        if (kV == 4) {
-          const float4 v = wk[k] == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : __ldcs(reinterpret_cast<const float4 *>(x));
-          f[k][0] = v.x; f[k][1] = v.y; f[k][2 % kV] = v.z; f[k][3 % kV] = v.w;
-        } else {
-          const float2 v = wk[k] == 0.f ? make_float2(0.f, 0.f) : __ldcs(reinterpret_cast<const float2 *>(x));
-          f[k][0] = v.x; f[k][1] = v.y;
+      for (int k = 0; k < kBatch; ++k) {
+        wk[k] = __shfl_sync(0xffffffffu, w, (k0 + k) & (kL - 1), kL);          // (kL is a multiple of kBatch)
+        const float *x = p.part + __shfl_sync(0xffffffffu, at, (k0 + k) & (kL - 1), kL) * D + lane * kVec;
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) {                // (an empty result holds no values at all)
+          if (kVec == 4) {
+            const float4 v = wk[k] == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : __ldcs(reinterpret_cast<const float4 *>(x + c * kL * kVec));
+            f[k][c * kVec] = v.x; f[k][c * kVec + 1] = v.y; f[k][c * kVec + 2 % kVec] = v.z; f[k][c * kVec + 3 % kVec] = v.w;
+          } else {
+            const float2 v = wk[k] == 0.f ? make_float2(0.f, 0.f) : __ldcs(reinterpret_cast<const float2 *>(x + c * kL * kVec));
+            f[k][c * kVec] = v.x; f[k][c * kVec + 1] = v.y;
+          }
         }
       }
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
+      for (int k = 0; k < kBatch; ++k) {
         den += wk[k];
 #pragma unroll
         for (int v = 0; v < kV; ++v) acc[v] = fmaf(wk[k], f[k][v], acc[v]);
       }
     }
   }
-  if (warps_a_row > 1) {                                   // the row's first warp adds the others' shares, in order
+  if (kL == 32 && warps_a_row > 1) {                       // the row's first warp adds the others' shares, in order
     if (share > 0) {
 #pragma unroll
       for (int v = 0; v < kV; ++v) others[warp][lane * kV + v] = acc[v];
@@ -1104,10 +1113,10 @@ ba_shared_merge_kernel(const __grid_constant__ SharedParams p, int warps_a_row) 
     __syncthreads();
     if (share > 0) return;
     for (int k = 1; k < warps_a_row; ++k) {
-      const float t = others[warp + k][32 * kV], d = others[warp + k][32 * kV + 1], mx = fmaxf(top, t);
+      const float t = others[warp + k][32 * kV], d = others[warp + k][32 * kV + 1];
       if (t == -INFINITY) continue;
-      rescale(mx);
-      const float f = __expf(t - mx);
+      rescale(fmaxf(top, t));
+      const float f = __expf(t - top);
       den = fmaf(d, f, den);
 #pragma unroll
       for (int v = 0; v < kV; ++v) acc[v] = fmaf(others[warp + k][lane * kV + v], f, acc[v]);
@@ -1117,15 +1126,19 @@ ba_shared_merge_kernel(const __grid_constant__ SharedParams p, int warps_a_row) 
   const float inv = den > 0.f ? 1.f / den : 0.f;
 #pragma unroll
   for (int v = 0; v < kV; ++v) acc[v] *= inv;
-  const long long out = here * D + lane * kV;
-  if (p.out_f32) {
-    float *o = reinterpret_cast<float *>(p.o) + out;
-    if (kV == 4) *reinterpret_cast<float4 *>(o) = make_float4(acc[0], acc[1], acc[2 % kV], acc[3 % kV]);
-    else *reinterpret_cast<float2 *>(o) = make_float2(acc[0], acc[1]);
-  } else {
-    __nv_bfloat16 *o = reinterpret_cast<__nv_bfloat16 *>(p.o) + out;
-    if (kV == 4) *reinterpret_cast<uint2 *>(o) = make_uint2(pack_bf16(acc[0], acc[1]), pack_bf16(acc[2 % kV], acc[3 % kV]));
-    else *reinterpret_cast<uint32_t *>(o) = pack_bf16(acc[0], acc[1]);
+#pragma unroll
+  for (int c = 0; c < kChunks; ++c) {
+    const long long out = here * D + c * kL * kVec + lane * kVec;
+    const float *a = acc + c * kVec;
+    if (p.out_f32) {
+      float *o = reinterpret_cast<float *>(p.o) + out;
+      if (kVec == 4) *reinterpret_cast<float4 *>(o) = make_float4(a[0], a[1], a[2 % kVec], a[3 % kVec]);
+      else *reinterpret_cast<float2 *>(o) = make_float2(a[0], a[1]);
+    } else {
+      __nv_bfloat16 *o = reinterpret_cast<__nv_bfloat16 *>(p.o) + out;
+      if (kVec == 4) *reinterpret_cast<uint2 *>(o) = make_uint2(pack_bf16(a[0], a[1]), pack_bf16(a[2 % kVec], a[3 % kVec]));
+      else *reinterpret_cast<uint32_t *>(o) = pack_bf16(a[0], a[1]);
+    }
   }
   if (p.lse && lane == 0) p.lse[here] = den > 0.f ? top + logf(den) : -INFINITY;
 }
@@ -1217,16 +1230,17 @@ ba_status ba_shared_prefix_attend(ba_ctx *ctx, const void *q, int32_t n_q_rows, 
   }
   const dim3 grid((unsigned)ctx->sm_count);
   const cudaStream_t cs = (cudaStream_t)stream;
-  // Few rows with long prefixes have more results than a warp wants to wait for (16 requests over 32000 tokens: 35 a row, 512 rows):
-  // four warps a row while that leaves the GPU room.
-  const int warps_a_row = (long long)n_q_rows * p.Hq <= 4096 ? 4 : 1;
-  const unsigned merge = (unsigned)(((long long)n_q_rows * p.Hq * warps_a_row + 7) / 8);
+  // (16 requests over 32000 tokens: 512 rows of 35 results; 24 questions: 30720 rows of four)
+  const long long rows_out = (long long)n_q_rows * p.Hq;
+  const bool wide = rows_out <= 16384;                     // (5120 rows of seven results: 9.7 us with a warp a row, 15.3 with eight lanes)
+  const int warps_a_row = rows_out <= 4096 ? 4 : 1;
+  const unsigned merge = (unsigned)((rows_out * warps_a_row * (wide ? 32 : 8) + 255) / 256);
   if (D == 128) {
     BA_CUDA_TRY(ba_launch(ba_shared_attend_kernel<128>, grid, kThreads, SharedLayout<128>::kBytes, cs, true, tkx, tvx, tk, tv, tq, p));
-    BA_CUDA_TRY(ba_launch(ba_shared_merge_kernel<128>, dim3(merge), 256, 0, cs, true, p, warps_a_row));
+    BA_CUDA_TRY(ba_launch(wide ? ba_shared_merge_kernel<128, 32> : ba_shared_merge_kernel<128, 8>, dim3(merge), 256, 0, cs, true, p, warps_a_row));
   } else {
     BA_CUDA_TRY(ba_launch(ba_shared_attend_kernel<64>, grid, kThreads, SharedLayout<64>::kBytes, cs, true, tkx, tvx, tk, tv, tq, p));
-    BA_CUDA_TRY(ba_launch(ba_shared_merge_kernel<64>, dim3(merge), 256, 0, cs, true, p, warps_a_row));
+    BA_CUDA_TRY(ba_launch(wide ? ba_shared_merge_kernel<64, 32> : ba_shared_merge_kernel<64, 8>, dim3(merge), 256, 0, cs, true, p, warps_a_row));
   }
   ctx->launches += 2;
   return BA_OK;

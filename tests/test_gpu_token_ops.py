@@ -341,6 +341,7 @@ CASES = {
     "items cut often": ([9000], [0, 3], [70, 1, 2], [100, 30, 2], 16, True),
     "many rows of their own": ([], [0], [50, 40], [1000, 2000], 64, True),
     "both kinds": ([40, 2000, 3], [0, 1, 2, 40], [3, 30] + [1] * 38, [100] * 40, 128, False),
+    "a thousand sequences": ([10, 300], [0, 3, 700], [1] * 1000, [(7 * i) % 33 for i in range(1000)], 16, False),
     "many": ([64, 200], [0, 70, 150], [1] * 150, [i % 140 for i in range(150)], 16, False),
 }
 
@@ -348,6 +349,8 @@ CASES = {
 @pytest.mark.parametrize("shape", [(4, 2, 64), (6, 2, 64), (8, 1, 128), (32, 8, 128), (3, 3, 128), (40, 1, 64)], ids=str)
 @pytest.mark.parametrize("name", list(CASES))
 def test_shared_attention(shape, name):
+    if name == "a thousand sequences" and shape[0] > 8:
+        pytest.skip("a minute of the oracle")
     b = Batch(shape, *CASES[name], seed=len(name), pad_rows=0 if name == "one token" else 2)
     c = make_context(shape, b)
     for out_dtype in (B.BA_OUT_F32, B.BA_OUT_BF16):
@@ -473,6 +476,116 @@ def test_rows_beyond_32_bits_of_elements():
     assert c.device_status() == B.BA_OK
     want, want_lse, size = tk.shared_attend(f64(q)[149:], lambda s: f64(k), lambda s: f64(v), [0, 1], [150], lambda s: 0, 128 ** -0.5)
     assert (np.abs(f64(o) - want) <= (HALF_STEP + 1e-4) * size).all() and (np.abs(f64(lse) - want_lse) <= 1e-4).all()
+    c.close()
+
+
+def test_one_pool_for_prefixes_and_sequences():
+    """Prefixes and own rows on lists of one pool, the prefix's pages shared with a sequence's list."""
+    shape = (8, 2, 128)
+    pool = [bf16(40 * 16, 2, 128, seed=s) for s in (1, 2)]
+    q = bf16(3, 8, 128, seed=3)
+    keep = ints([0, 5]), ints([3, 9, 4, 11, 0]), ints([0, 2, 4, 9]), ints([20, 21, 30, 31, 3, 9, 4, 11, 0])
+    cfg = B.ba_config(*shape, 0, 1e4, 0.0, 0)
+    c = R.Context(*shape, 1e4, max_blocks=64, max_q_rows=64, workspace_bytes=B.ba_shared_prefix_bytes(cfg, 3, 1, 3))
+    tables = ints([0, 2]), ints([0, 70]), ints([17, 32, 75])
+    o, lse = torch.empty(3, 8, 128, device="cuda"), torch.empty(3, 8, device="cuda")
+    B.ba_shared_prefix_attend(c.ctx, q, 3, *pool, 0, B.make_page_table(16, 40, *keep[:2]), *pool, B.make_page_table(16, 40, *keep[2:]),
+                              B.make_shared_batch(3, 1, tables[0], tables[1], None, tables[2]), o, lse, B.BA_OUT_F32)
+    assert c.device_status() == B.BA_OK
+    prefix = tk.page_rows_of([0, 5], [3, 9, 4, 11, 0], 16, 0, 70)
+    own = [tk.page_rows_of([0, 2, 4, 9], [20, 21, 30, 31, 3, 9, 4, 11, 0], 16, s, n) for s, n in enumerate((17, 32, 75))]
+    rows = [prefix + own[0], prefix + own[1], own[2]]
+    want, want_lse, size = tk.shared_attend(f64(q), lambda s: f64(pool[0])[rows[s]], lambda s: f64(pool[1])[rows[s]], [0, 1, 2, 3], [17, 32, 75],
+                                            lambda s: 70 if s < 2 else 0, 128 ** -0.5)
+    assert (np.abs(f64(o) - want) <= (HALF_STEP + 1e-4) * size).all() and (np.abs(f64(lse) - want_lse) <= 1e-4).all()
+    c.close()
+
+
+def test_what_lies_in_padding_rows_changes_nothing():
+    """Query rows behind the last sequence share a tile with real ones: other values there, the same bits everywhere else."""
+    b = Batch((8, 2, 128), [400, 900], [0, 20, 25], [1] * 25, [40] * 25, 16, False, seed=5, pad_rows=30)
+    c = make_context((8, 2, 128), b)
+    outs = []
+    for fill in (0.0, 40.0, float("nan"), float("inf")):
+        b.q[25:] = fill
+        o, lse = torch.zeros(55, 8, 128, device="cuda"), torch.zeros(55, 8, device="cuda")
+        b.call(c, o, lse, B.BA_OUT_F32)
+        outs.append((o, lse))
+    for o, lse in outs[1:]:
+        assert torch.equal(o, outs[0][0]) and torch.equal(lse, outs[0][1])
+    c.close()
+
+
+def test_a_captured_decode_step():
+    """Append and attention captured together and replayed: the tables move on between replays, as a server's would."""
+    shape = (8, 2, 64)
+    hq, hkv, d = shape
+    cfg = B.ba_config(*shape, 0, 1e4, 0.0, 0)
+    c = R.Context(*shape, 1e4, max_blocks=64, max_q_rows=64, workspace_bytes=B.ba_shared_prefix_bytes(cfg, 4, 1, 4))
+    prefix = [bf16(300, hkv, d, seed=s) for s in (1, 2)]
+    cu, idx, n_pages, table, keep = page_lists([40] * 4, 16)
+    pools = [torch.full((n_pages * 16, hkv, d), float("nan"), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    qkv, q_out = bf16(4, hq + 2 * hkv, d, seed=3), torch.empty(4, hq, d, dtype=torch.bfloat16, device="cuda")
+    w = bf16(d, seed=4)
+    pos, start, own, prefix_cu = ints([300] * 4), ints([0] * 4), ints([1] * 4), ints([0, 300])
+    shared = B.make_shared_batch(4, 1, None, prefix_cu, None, own)
+    o, lse = torch.empty(4, hq, d, device="cuda"), torch.empty(4, hq, device="cuda")
+
+    def step():
+        B.ba_append_paged(c.ctx, qkv[:, :hq], qkv[:, hq:hq + hkv], qkv[:, hq + hkv:], 4, pos, w, w, 1e-6, None, start, 4, q_out, *pools, table)
+        B.ba_shared_prefix_attend(c.ctx, q_out, 4, *prefix, 300, None, *pools, table, shared, o, lse, B.BA_OUT_F32)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        step()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        step()
+    keys, values = [f64(prefix[0])], [f64(prefix[1])]
+    for n in range(20):
+        qkv.copy_(bf16(4, hq + 2 * hkv, d, seed=100 + n))
+        pos.fill_(300 + n)
+        start.fill_(n)
+        own.fill_(n + 1)
+        graph.replay()
+        assert c.device_status() == B.BA_OK
+        at = [tk.page_rows_of(cu, idx, 16, s, n + 1) for s in range(4)]
+        want, want_lse, size = tk.shared_attend(f64(q_out), lambda s: np.concatenate([keys[0], f64(pools[0])[at[s]]]),
+                                                lambda s: np.concatenate([values[0], f64(pools[1])[at[s]]]), [0, 1, 2, 3, 4], [n + 1] * 4, lambda s: 300,
+                                                d ** -0.5)
+        assert torch.equal(pools[1][[a[-1] for a in at]], qkv[:, hq + hkv:])
+        assert (np.abs(f64(o) - want) <= (HALF_STEP + 1e-4) * size).all() and (np.abs(f64(lse) - want_lse) <= 1e-4).all()
+    c.close()
+
+
+def test_the_calls_without_the_extension(monkeypatch):
+    """Through ctypes: the same bits as through the extension."""
+    shape = (6, 2, 64)
+    hq, hkv, d = shape
+    cfg = B.ba_config(*shape, 0, 1e4, 0.0, 0)
+    c = R.Context(*shape, 1e4, max_blocks=64, max_q_rows=64, workspace_bytes=B.ba_shared_prefix_bytes(cfg, 3, 0, 3))
+    qkv, w = bf16(3, hq + 2 * hkv, d, seed=3), bf16(d, seed=4)
+    q, k, v = qkv[:, :hq], qkv[:, hq:hq + hkv], qkv[:, hq + hkv:]
+    cu, idx, n_pages, table, keep = page_lists([5, 20, 40], 16)
+    start, own, pos = ints([4, 19, 39]), ints([5, 20, 40]), ints([9, 8, 7])
+    shared = B.make_shared_batch(3, 0, None, None, None, own)
+
+    def everything():
+        pools = [bf16(n_pages * 16, hkv, d, seed=s) for s in (1, 2)]
+        q_out, o, lse = torch.empty(3, hq, d, dtype=torch.bfloat16, device="cuda"), torch.empty(3, hq, d, device="cuda"), torch.empty(3, hq, device="cuda")
+        B.ba_append_paged(c.ctx, q, k, v, 3, pos, w, w, 1e-6, None, start, 3, q_out, *pools, table)
+        B.ba_shared_prefix_attend(c.ctx, q_out, 3, None, None, 0, None, *pools, table, shared, o, lse, B.BA_OUT_F32)
+        qn, kn = torch.empty(3, hq, d, dtype=torch.bfloat16, device="cuda"), torch.empty(3, hkv, d, dtype=torch.bfloat16, device="cuda")
+        B.ba_qk_norm_rope(c.ctx, q, k, 3, pos, w, w, 1e-6, qn, kn)
+        grad = torch.zeros(3, hq + 2 * hkv, d, dtype=torch.bfloat16, device="cuda")
+        dw = torch.empty(2, d, device="cuda")
+        B.ba_qk_norm_rope_bwd(c.ctx, q, k, 3, pos, w, w, 1e-6, qn, kn, grad[:, :hq], grad[:, hq:hq + hkv], dw[0], dw[1], B.BA_OUT_BF16)
+        return [*pools, q_out, o, lse, qn, kn, grad, dw]
+    fast = everything()
+    monkeypatch.setattr(B, "_marshal", B._CtypesCalls())
+    for a, b in zip(fast, everything()):
+        assert torch.equal(a, b)
+    assert c.device_status() == B.BA_OK
     c.close()
 
 
