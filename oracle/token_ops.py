@@ -75,14 +75,15 @@ def shared_attend(q, keys_of, values_of, q_cu, own_len, prefix_len_of, scale):
         G = hq // k.shape[1]
         for i in range(a, b):
             n = prefix_len_of(s) + max(0, int(own_len[s]) - (b - 1 - i))
-            for h in range(hq):
-                if n == 0:
-                    o[i, h], lse[i, h], size[i, h] = 0.0, -np.inf, 0.0
-                    continue
-                z = scale * (k[:n, h // G] @ q[i, h])
-                top = z.max()
+            if n == 0:
+                o[i], lse[i], size[i] = 0.0, -np.inf, 0.0
+                continue
+            for h in range(k.shape[1]):                       # the query heads of a KV head together
+                heads = slice(h * G, (h + 1) * G)
+                z = scale * (q[i, heads] @ k[:n, h].T)
+                top = z.max(1, keepdims=True)
                 p = np.exp(z - top)
-                lse[i, h] = top + np.log(p.sum())
-                p /= p.sum()
-                o[i, h], size[i, h] = p @ v[:n, h // G], p @ np.abs(v[:n, h // G])
+                den = p.sum(1, keepdims=True)
+                lse[i, heads] = (top + np.log(den))[:, 0]
+                o[i, heads], size[i, heads] = p / den @ v[:n, h], p / den @ np.abs(v[:n, h])
     return o, lse, size

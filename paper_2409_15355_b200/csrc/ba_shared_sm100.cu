@@ -17,7 +17,8 @@
 // each, with mma.sync on operands from shared memory: S = Q K^T, softmax with maxima and sums of the warp's own keys, O += P V with P from
 // registers.  The warps share nothing until the end of a piece, where their maxima, sums and accumulators are merged.
 // Many rows: tcgen05 with accumulators in tensor memory, warps 0-3 and 4-7 softmax (a thread a row), warps 8 and 10 copy keys
-// and values, warp 9 issues the products, warp 11 fetches queries.  Items of more than 128 rows: the two softmax groups have a tile of queries each and share key
+// (and queries) and values, warp 9 issues the products (a thread for each softmax group: their products get into one another's way, 24 questions
+// over 16384 tokens 308 -> 329 us).  Items of more than 128 rows: the two softmax groups have a tile of queries each and share key
 // tiles; items of fewer: they share the query tile and take key tiles in turn, each with an accumulator of its own, so that products and
 // exponentials overlap there too; the merge counts them as two results.
 //
@@ -573,13 +574,44 @@ __device__ __forceinline__ void many_rows(const SharedParams &p, const CUtensorM
     any_pair = any_pair || (ctrl->pairs[e >> 5] >> (e & 31) & 1);
   const KeyRing<D> keys = {!any_pair};
   if (warp == 8) {
-    // ------------------------------------------------------------ copies of keys
+    // ------------------------------------------------------------ copies of queries and keys
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kServiceRegs));
-    int nk = 0;                                            // tiles requested so far
+    int nk = 0, n_pieces = 0, n_q = 0;                     // key tiles requested, pieces begun; pieces whose queries the copy engine fetches
     for (int at = begin; at < end && ok;) {
       const Piece k = piece_at(p, units, n_entries, at, end);
       at += k.units;
       if (k.n == 0) continue;
+      // the queries, once the piece before has no use for their place
+      auto load_queries = [&]() -> bool {
+        if (!__all_sync(0xffffffffu, mbar_wait(&ctrl->q_empty, (n_pieces & 1) ^ 1, abort_flag))) return false;
+        ++n_pieces;
+        const int tile_rows = k.n_rows > 128 ? 256 : 128;
+        if (p.q_boxes) {                                   // the heads of a group divide a tile: boxes of whole tokens
+          if (lane == 0) {
+            mbar_arrive_expect_tx(&ctrl->q_full, tile_rows * D * 2);
+            for (int t = 0; t * 128 < tile_rows; ++t)
+              for (int c = 0; c < D / 64; ++c)
+                tma_load_3d(smem + t * L::kTileBytes + c * L::kRegion, tmap_q, &ctrl->q_full, c * 64, k.head * p.G, k.x.q_row0 + (k.row0 + t * 128) / p.G);
+          }
+          n_q = n_pieces;
+        } else {                                           // 16 bytes a copy, into the tiles' swizzled layout
+          constexpr int kVecs = D / 8;
+          const int c = lane % kVecs;
+          const RowMap map(p, k.x, k.row0, k.head);
+          const uint32_t base = smem_u32(smem) + (c >> 3) * L::kRegion;
+#pragma unroll 8
+          for (int r = lane / kVecs; r < tile_rows; r += 32 / kVecs) {
+            const bool there = r < k.n_rows;               // (rows that are not there are zeros)
+            copy_16_or_zero(base + (r >> 7) * L::kTileBytes + (r & 127) * 128 + (((c & 7) ^ (r & 7)) << 4), p.q + map.row(there ? r : 0) * D + c * 8, there);
+          }
+          asm volatile("cp.async.wait_all;" ::: "memory");
+          fence_proxy_async();                             // the tensor core reads through the async proxy
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&ctrl->q_full);
+        }
+        __syncwarp();
+        return true;
+      };
       const Source src = source_of(p, k);
       int next = box_row(p, src, k.tile0);                 // (looked up a tile ahead)
       for (int j = 0; j < k.n; ++j, ++nk) {
@@ -588,13 +620,18 @@ __device__ __forceinline__ void many_rows(const SharedParams &p, const CUtensorM
         ok = __all_sync(0xffffffffu, mbar_wait(&k_empty[st], keys.phase(nk) ^ 1, abort_flag));
         if (!ok) break;
         copy_tile<D>(src, k.e >= p.n_groups ? tmap_k : tmap_kx, smem + KeyRing<D>::offset(st), &k_full[st], k.head, row);
+        if (j == 0) ok = load_queries();                   // (behind the first keys, whose place is free sooner)
+        if (!ok) { ++nk; break; }
       }
     }
     if (!ok) {
-      // leave no copy in flight: wait (bounded) for the tiles already requested
+      // leave no copy in flight: wait (bounded) for what was requested
       for (int i = max(0, nk - keys.depth()); i < nk; ++i)
         for (uint32_t spin = 0; spin < (1u << 20); ++spin)
           if (mbar_try_wait(&k_full[keys.stage(i)], keys.phase(i))) break;
+      if (n_q > 0)
+        for (uint32_t spin = 0; spin < (1u << 20); ++spin)
+          if (mbar_try_wait(&ctrl->q_full, (n_q - 1) & 1)) break;
     }
   } else if (warp == 9) {
     // ------------------------------------------------------------ products
@@ -670,46 +707,14 @@ __device__ __forceinline__ void many_rows(const SharedParams &p, const CUtensorM
         nk += n; nv += n;
       }
     }
-  } else if (warp >= 10) {
-    // ------------------------------------------------------------ warp 10: copies of values; warp 11, and both for the first piece: queries
+  } else if (warp == 10) {
+    // ------------------------------------------------------------ copies of values
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kServiceRegs));
-    const bool values = warp == 10;
-    int nv = 0, n_pieces = 0, n_q = 0;                     // tiles and pieces so far; of those, with queries fetched by the copy engine
+    int nv = 0;
     for (int at = begin; at < end && ok;) {
       const Piece k = piece_at(p, units, n_entries, at, end);
       at += k.units;
       if (k.n == 0) continue;
-      if (!values) ok = __all_sync(0xffffffffu, mbar_wait(&ctrl->q_empty, (n_pieces & 1) ^ 1, abort_flag));
-      if (!ok) break;
-      const int tile_rows = k.n_rows > 128 ? 256 : 128;
-      if (p.q_boxes) {                                     // the heads of a group divide a tile: boxes of whole tokens
-        if (!values && lane == 0) {
-          mbar_arrive_expect_tx(&ctrl->q_full, tile_rows * D * 2);
-          for (int t = 0; t * 128 < tile_rows; ++t)
-            for (int c = 0; c < D / 64; ++c)
-              tma_load_3d(smem + t * L::kTileBytes + c * L::kRegion, tmap_q, &ctrl->q_full, c * 64, k.head * p.G, k.x.q_row0 + (k.row0 + t * 128) / p.G);
-        }
-        __syncwarp();
-        n_q = n_pieces + 1;
-      } else if (!values || n_pieces == 0) {               // 16 bytes a copy, into the tiles' swizzled layout
-        constexpr int kVecs = D / 8;
-        const int thread = n_pieces == 0 ? (int)threadIdx.x - 320 : lane, threads = n_pieces == 0 ? 64 : 32;
-        const int c = thread % kVecs;
-        const RowMap map(p, k.x, k.row0, k.head);
-        const uint32_t base = smem_u32(smem) + (c >> 3) * L::kRegion;
-#pragma unroll 8
-        for (int r = thread / kVecs; r < tile_rows; r += threads / kVecs) {
-          const bool there = r < k.n_rows;                 // (rows that are not there are zeros)
-          copy_16_or_zero(base + (r >> 7) * L::kTileBytes + (r & 127) * 128 + (((c & 7) ^ (r & 7)) << 4), p.q + map.row(there ? r : 0) * D + c * 8, there);
-        }
-        asm volatile("cp.async.wait_all;" ::: "memory");
-        fence_proxy_async();                               // the tensor core reads through the async proxy
-        if (n_pieces == 0) asm volatile("bar.sync 2, 64;" ::: "memory");       // (no wait of either warp before it can expire)
-        else __syncwarp();
-        if (!values && lane == 0) mbar_arrive(&ctrl->q_full);
-      }
-      ++n_pieces;
-      if (!values) continue;
       const Source src = source_of(p, k);
       int next = box_row(p, src, k.tile0);
       for (int j = 0; j < k.n; ++j, ++nv) {
@@ -720,14 +725,13 @@ __device__ __forceinline__ void many_rows(const SharedParams &p, const CUtensorM
         copy_tile<D>(src, k.e >= p.n_groups ? tmap_v : tmap_vx, smem + L::kValues + st * L::kTileBytes, &v_full[st], k.head, row);
       }
     }
-    if (!ok && !values && n_q > 0)                         // leave no copy in flight: wait (bounded) for what was requested
-      for (uint32_t spin = 0; spin < (1u << 20); ++spin)
-        if (mbar_try_wait(&ctrl->q_full, (n_q - 1) & 1)) break;
-    if (!ok && values) {
+    if (!ok) {
       for (int i = max(0, nv - kDepth); i < nv; ++i)
         for (uint32_t spin = 0; spin < (1u << 20); ++spin)
           if (mbar_try_wait(&v_full[i % kDepth], (i / kDepth) & 1)) break;
     }
+  } else if (warp == 11) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kServiceRegs));
   } else {
     // ------------------------------------------------------------ softmax, a thread a row
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));

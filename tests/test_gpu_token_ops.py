@@ -295,11 +295,13 @@ class Batch:
                                   lse, out_dtype, stream)
 
     def reference(self, scale):
+        pool, prefix = [f64(p) for p in self.pool], [f64(p) for p in self.kv_prefix]
+
         def rows(i):
             def of(s):
-                own = f64(self.pool[i])[tk.page_rows_of(self.cu, self.idx, self.page_rows, s, self.own[s])]
+                own = pool[i][tk.page_rows_of(self.cu, self.idx, self.page_rows, s, self.own[s])]
                 g = self.group[s]
-                return own if g < 0 else np.concatenate([f64(self.kv_prefix[i])[self.prefix_rows[g]], own])
+                return own if g < 0 else np.concatenate([prefix[i][self.prefix_rows[g]], own])
             return of
         return tk.shared_attend(f64(self.q)[:self.rows], rows(0), rows(1), self.q_cu, self.own,
                                 lambda s: self.prefix[self.group[s]] if self.group[s] >= 0 else 0, scale)
