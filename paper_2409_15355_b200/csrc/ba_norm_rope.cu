@@ -10,6 +10,9 @@
 // thread keeps one side's weights and sums.  One (cos, sin) pair of a row serves all of its heads: a warp that has a row folds its four
 // pairs a lane into the weights and walks the heads; with few rows the heads of a row are shared out among warps instead.  The values
 // of two rotary pairs are kept side by side, first members and second members, for arithmetic on two floats at a time.
+//
+// Measured, heads of 128: 131072 rows of 32 + 8 heads 476 us (5.65 TB/s, 86 % of a copy), their gradients at 32768 rows 190 us (5.3 TB/s) and
+// 5 us for the weights' sums; 64 passages of 1000 rows into pages 109 us (4.8 TB/s); one row each of 16 sequences 4 us.
 #include <string.h>
 
 #include <algorithm>
@@ -27,8 +30,10 @@ namespace {
 
 constexpr int kNormThreads = 256;
 constexpr int kNormWarps = kNormThreads / 32;
-constexpr int kAhead = 4, kBwdAhead = 4;  // steps in flight
-constexpr int kFwdCtas = 3, kBwdCtas = 2; // CTAs an SM has room for
+// Steps in flight a warp, and CTAs an SM: more of the one leave registers for fewer of the other.  131072 rows, us: 4 x 3 476, 4 x 4 482, 3 x 4 508,
+// 2 x 5 555, 8 x 2 629; gradients of 32768 rows: 4 x 2 190, 2 x 2 221, 1 x 4 227, 2 x 3 254, 3 x 3 315.
+constexpr int kAhead = 4, kBwdAhead = 4;
+constexpr int kFwdCtas = 3, kBwdCtas = 2;
 
 // One side of a call: rows of `heads` heads, `stride` elements apart.
 struct NormSide {
@@ -202,7 +207,7 @@ __device__ __forceinline__ float head_sum(float x) {
 }
 
 // Places of rows in their sequences' page lists -> pool rows, for a warp that walks rows one behind the other: tables are looked up where a
-// sequence or a page begins (64 passages of 1000 tokens, looked up for every row: 123 us, so 90).
+// sequence or a page begins (64 passages of 1000 tokens, looked up for every row: 123 us, so 109).
 struct AppendWalk {
   int s = -1, first = 0, end = 0;        // sequence, its rows
   int list = 0, n_list = 0;              // its pages

@@ -22,6 +22,10 @@
 // tiles; items of fewer: they share the query tile and take key tiles in turn, each with an accumulator of its own, so that products and
 // exponentials overlap there too; the merge counts them as two results.
 //
+// Measured, 32 heads over 8 KV heads of 128: 64 sequences of 1500-7000 rows of their own 160 us of kernel for 161 of the bytes at a copy's rate;
+// 16 sequences of one token over a prefix of 32000 keys 36 us (20 of them the prefix's bytes); 24 questions of 17-64 tokens over 16384 keys 280 us,
+// 50 % of the tensor pipe: a pair of tiles takes 3270 cycles, its products 2100, the chain from scores over softmax to scores is what is left.
+//
 // Rounding: P to bf16 (the products' type; 2^-8 relative at most, the sums of the softmax are taken before it), o once at the end.
 #include <algorithm>
 
@@ -814,7 +818,8 @@ __device__ __forceinline__ void many_rows(const SharedParams &p, const CUtensorM
         for (int i = 0; i < 16; ++i) expo(64 + 2 * i, pk1[i], i);
         const int valid = k.x.len - key0;
         if (valid < kTile) {
-          // values behind the end may be anything, and zero times a NaN is a NaN: zeros there, before the product may start
+          // values behind the end may be anything, and zero times a NaN is a NaN: zeros there, before the product may start.  (These
+          // scores were issued after the products with what lay in that stage before, so that the barrier's phase is the one meant.)
           const int jv = nv + j;
           ok = __all_sync(0xffffffffu, mbar_wait(&v_full[jv % kDepth], (jv / kDepth) & 1, abort_flag));
           if (!ok) break;
