@@ -70,7 +70,11 @@ class ba_shared_batch(C.Structure):
 
 
 def make_shared_batch(batch: int, n_groups: int, group_cu, prefix_cu, q_cu, own_len) -> "ba_shared_batch":
-    """group_cu / prefix_cu / q_cu / own_len: torch int32 CUDA tensors (kept alive by the caller) or None (see include/ba.h)."""
+    """group_cu / prefix_cu / q_cu / own_len: torch int32 CUDA tensors (kept alive by the caller), their addresses, or None (see
+    include/ba.h)."""
+    for t in (group_cu, prefix_cu, q_cu, own_len):
+        if t is not None and not isinstance(t, int) and (not getattr(t, "is_cuda", False) or str(t.dtype) != "torch.int32"):
+            raise ValueError("the tables of a shared batch are int32 tensors on the device")
     return ba_shared_batch(batch, n_groups, _ptr(group_cu), _ptr(prefix_cu), _ptr(q_cu), _ptr(own_len))
 
 

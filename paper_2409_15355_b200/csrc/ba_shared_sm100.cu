@@ -145,8 +145,10 @@ __device__ __forceinline__ bool load_entry(const SharedParams &p, int e, Entry &
     if (len < 0 || len > room) return false;
     a = s; b = s + 1; x.len = len;
   }
-  x.q_row0 = q_begin(p, a); x.rows = q_begin(p, b) - x.q_row0;
-  return x.q_row0 >= 0 && x.rows >= 0 && x.q_row0 + x.rows <= p.n_q_rows;
+  const int first = q_begin(p, a), last = q_begin(p, b);   // (their difference may not fit where they do not hold)
+  if (first < 0 || last < first || last > p.n_q_rows || x.len > INT32_MAX - 2 * kTile) { x.len = 0; return false; }
+  x.q_row0 = first; x.rows = last - first;
+  return true;
 }
 __device__ __forceinline__ int tiles_of(const Entry &x) { return (x.len + kTile - 1) / kTile; }
 __device__ __forceinline__ bool is_many(const SharedParams &p, const Entry &x) { return x.rows * p.G > kRows; }

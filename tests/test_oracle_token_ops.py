@@ -129,6 +129,13 @@ def test_structures_are_not_mixed_up():
                                   stream=_Stream)
 
 
+def test_tables_on_the_host_are_refused():
+    import torch
+    for bad in (np.zeros(2, dtype=np.int32), torch.zeros(2, dtype=torch.int32), [0, 1]):
+        with pytest.raises(ValueError):
+            B.make_shared_batch(1, 1, None, bad, None, 0x1000)
+
+
 def test_views_whose_heads_lie_apart_are_refused():
     import torch
     x = torch.zeros(4, 8, 64, dtype=torch.bfloat16)
