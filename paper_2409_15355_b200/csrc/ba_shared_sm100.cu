@@ -1005,7 +1005,7 @@ ba_shared_attend_kernel(const __grid_constant__ CUtensorMap tmap_kx, const __gri
 }
 
 // The partial results of every (row, head): those of its group's prefix and of its own rows, weighted by their denominators.  What a row
-// waits for is a chain of look-ups, so rows go side by side: eight lanes a row (30720 rows: 34 us with a warp each), or, with few rows,
+// waits for is a chain of look-ups, so rows go side by side: eight lanes a row (32600 rows: 34 us with a warp each), or, with few rows,
 // whose long prefixes leave many results, a warp or several.
 template <int D, int kL>
 __global__ void __launch_bounds__(256)
@@ -1241,7 +1241,7 @@ ba_status ba_shared_prefix_attend(ba_ctx *ctx, const void *q, int32_t n_q_rows, 
   }
   const dim3 grid((unsigned)ctx->sm_count);
   const cudaStream_t cs = (cudaStream_t)stream;
-  // (16 requests over 32000 tokens: 512 rows of 35 results; 24 questions: 30720 rows of four)
+  // (16 requests over 32000 tokens: 512 rows of 35 results; 24 questions: 32600 rows of four)
   const long long rows_out = (long long)n_q_rows * p.Hq;
   const bool wide = rows_out <= 16384;                     // (5120 rows of seven results: 9.7 us with a warp a row, 15.3 with eight lanes)
   const int warps_a_row = rows_out <= 4096 ? 4 : 1;
