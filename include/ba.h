@@ -494,7 +494,7 @@ typedef struct {
  * What lies behind the end of a prefix, a sequence or a list in pages or rows is never used and may hold any bits.  A page number outside
  * its pool counts as zeros and is reported (BA_ERR_INVALID_ARG).  Tables that do not fit together (a cumulative table that decreases
  * or leaves its range, a length below zero or above its list's pages) are reported the same way and nothing is written; so is an
- * amount of work beyond any memory (key tiles of 128 x KV heads x 256 query rows of one entry above five million).
+ * amount of work beyond any launch (key tiles of 128 x KV heads x 256 query rows of all entries above six hundred million).
  * Uses ba_shared_prefix_bytes() bytes of workspace at most (to be given to ba_create(); BA_ERR_WORKSPACE otherwise); batch + n_groups is
  * at most BA_SHARED_MAX (BA_ERR_UNSUPPORTED).  No atomics: results are run-to-run identical.
  */

@@ -53,7 +53,7 @@ constexpr int kSoftmaxRegs = 208, kServiceRegs = 88;     // of CTAs for many row
 constexpr int kTileFew = 1, kTilePair = 3, kTileSolo = 2, kFrontFew = 4, kFrontMany = 10;
 // What a unit costs, to share out the CTAs between the streams.
 constexpr float kCostFew = 3.f, kCostMany = 2.f;
-constexpr int kMostUnits = INT32_MAX / kThreads;           // of one thread's entries: the sums stay in 32 bits
+constexpr long long kMostUnits = 2000000000;               // of a stream: places in it are 32 bits
 constexpr float kRescale = 8.f;       // O is rescaled when a maximum grows by more than 2^8: exact in real arithmetic, values stay bounded
 
 struct SharedParams {
@@ -109,7 +109,7 @@ struct SharedCtrl {
   uint32_t tmem_base;
   uint32_t prefixed[kMaxEntries / 32];         // a bit a sequence: it has a prefix
   uint32_t pairs[kMaxEntries / 32];   // a bit an entry: it has items of more than 128 rows
-  int2 warp_sums[kThreads / 32];      // units of few rows, of many
+  longlong2 warp_sums[kThreads / 32]; // units of few rows, of many
 };
 static_assert(sizeof(SharedCtrl) <= kCtrlBytes, "control area");
 
@@ -928,14 +928,11 @@ ba_shared_attend_kernel(const __grid_constant__ CUtensorMap tmap_kx, const __gri
   ba_pdl_trigger();
   // The streams: units before every entry, by kind, and what the entries of many rows cost.  A thread takes neighbouring entries.
   const int per = (n_entries + kThreads - 1) / kThreads, e0 = min(n_entries, tid * per), e1 = min(n_entries, e0 + per);
-  int sum[2] = {0, 0};
+  long long sum[2] = {0, 0};
   Entry one;                                               // (a thread's only entry, where there are no more than threads)
   for (int e = e0; e < e1; ++e) {
-    bool good = load_entry(p, e, one);
-    const long long n = lay_of(p, one).a_head() * p.Hkv;
-    good = good && sum[0] + sum[1] + n <= kMostUnits;
-    if (!good) { ctrl->invalid = 1; break; }
-    sum[is_many(p, one)] += (int)n;
+    if (!load_entry(p, e, one)) { ctrl->invalid = 1; break; }
+    sum[is_many(p, one)] += lay_of(p, one).a_head() * p.Hkv;
     if (one.rows * p.G > 128) atomicOr(&ctrl->pairs[e >> 5], 1u << (e & 31));
     if (e < p.n_groups && one.len > 0) {                   // its sequences do not write their rows straight to the output
       const int a = p.group_cu ? __ldg(p.group_cu + e) : 0, b = p.group_cu ? __ldg(p.group_cu + e + 1) : p.batch;
@@ -945,22 +942,22 @@ ba_shared_attend_kernel(const __grid_constant__ CUtensorMap tmap_kx, const __gri
       }
     }
   }
-  const int mine[2] = {sum[0], sum[1]};
+  const long long mine[2] = {sum[0], sum[1]};
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
-    const int a = __shfl_up_sync(0xffffffffu, sum[0], d), b = __shfl_up_sync(0xffffffffu, sum[1], d);
+    const long long a = __shfl_up_sync(0xffffffffu, sum[0], d), b = __shfl_up_sync(0xffffffffu, sum[1], d);
     if (lane >= d) { sum[0] += a; sum[1] += b; }
   }
-  if (lane == 31) ctrl->warp_sums[warp] = make_int2(sum[0], sum[1]);
+  if (lane == 31) ctrl->warp_sums[warp] = make_longlong2(sum[0], sum[1]);
   __syncthreads();
-  int total[2] = {0, 0};
+  long long total[2] = {0, 0};
 #pragma unroll
   for (int w = 0; w < kThreads / 32; ++w) {
-    const int2 v = ctrl->warp_sums[w];
+    const longlong2 v = ctrl->warp_sums[w];
     if (w < warp) { sum[0] += v.x; sum[1] += v.y; }
     total[0] += v.x; total[1] += v.y;
   }
-  const bool valid = !ctrl->invalid;
+  const bool valid = !ctrl->invalid && total[0] <= kMostUnits && total[1] <= kMostUnits;
   // CTAs for many rows
   int n_many = 0;
   if (valid && total[1] > 0) {
@@ -972,10 +969,10 @@ ba_shared_attend_kernel(const __grid_constant__ CUtensorMap tmap_kx, const __gri
   // (a run is a tile at least: every CTA between an item's first and last tile has one of it)
   auto run_of = [&](int kind) {
     const unsigned n = (unsigned)(kind ? n_many : n_few);
-    return valid && n > 0 ? max(kind ? kTilePair : kTileFew, (int)(((unsigned)total[kind] + n - 1) / n)) : 0;
+    return valid && n > 0 ? max(kind ? kTilePair : kTileFew, (int)(((unsigned)total[kind] + n - 1) / n)) : 0;     // (fits: total is checked)
   };
   if (valid) {
-    int u[2] = {sum[0] - mine[0], sum[1] - mine[1]};
+    int u[2] = {(int)(sum[0] - mine[0]), (int)(sum[1] - mine[1])};
     for (int e = e0; e < e1; ++e) {
       units[e] = u[0]; units_many[e] = u[1];
       const Entry x = per == 1 ? one : get_entry(p, e);
@@ -983,16 +980,16 @@ ba_shared_attend_kernel(const __grid_constant__ CUtensorMap tmap_kx, const __gri
       if (blockIdx.x == 0) p.meta[e] = make_int4(u[many], tiles_of(x), x.rows * p.G, many);
       u[many] += (int)lay_of(p, x).a_head() * p.Hkv;
     }
-    if (tid == kThreads - 1) { units[n_entries] = total[0]; units_many[n_entries] = total[1]; }
+    if (tid == kThreads - 1) { units[n_entries] = (int)total[0]; units_many[n_entries] = (int)total[1]; }
   }
   if (blockIdx.x == 0 && tid == 0) {
     p.meta[n_entries] = make_int4(run_of(0), run_of(1), n_many, valid);
     if (!valid) ba_record_status(p.status, BA_ERR_INVALID_ARG);
   }
   const bool many = (int)blockIdx.x < n_many;
-  const int nth = many ? (int)blockIdx.x : (int)blockIdx.x - n_many, all = valid ? total[many] : 0;
+  const int nth = many ? (int)blockIdx.x : (int)blockIdx.x - n_many, all = valid ? (int)total[many] : 0;
   const int run = run_of(many);
-  const int begin = (int)min((long long)all, (long long)run * nth), end = min(all, begin + run);
+  const int begin = (int)min((long long)all, (long long)run * nth), end = (int)min((long long)all, (long long)begin + run);
   __syncthreads();
   if (begin < end) {
     if (many) many_rows<D>(p, &tmap_kx, &tmap_vx, &tmap_k, &tmap_v, &tmap_q, smem, ctrl, units_many, n_entries, begin, end);
