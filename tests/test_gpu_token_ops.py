@@ -558,6 +558,52 @@ def test_a_captured_decode_step():
     c.close()
 
 
+def test_two_contexts_on_two_streams():
+    """Calls of two contexts that run at the same time: each gives what it gives alone."""
+    batches = [Batch((8, 2, 128), [3000, 200], [0, 20, 30], [1] * 40, [500] * 40, 16, False, seed=5), Batch((8, 2, 128), [900], [0, 3], [40, 1, 7], [40, 300, 90], 64, True, seed=6)]
+    contexts = [make_context((8, 2, 128), b) for b in batches]
+    alone = []
+    for b, c in zip(batches, contexts):
+        o, lse = torch.empty(b.rows, 8, 128, device="cuda"), torch.empty(b.rows, 8, device="cuda")
+        b.call(c, o, lse, B.BA_OUT_F32)
+        alone.append((o, lse))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in batches]
+    outs = [[(torch.empty_like(a[0]), torch.empty_like(a[1])) for _ in range(10)] for a in alone]
+    torch.cuda.synchronize()
+    for n in range(10):
+        for b, c, st, out in zip(batches, contexts, streams, outs):
+            b.call(c, *out[n], B.BA_OUT_F32, st)
+    torch.cuda.synchronize()
+    for a, out in zip(alone, outs):
+        for o, lse in out:
+            assert torch.equal(o, a[0]) and torch.equal(lse, a[1])
+    for c in contexts:
+        assert c.device_status() == B.BA_OK
+        c.close()
+
+
+def test_a_queued_reencoding_stays_queued():
+    """The calls leave a deferred re-encoding and its table at the end of the workspace alone."""
+    b = Batch((8, 2, 128), [200], [0, 3], [1] * 4, [50] * 4, 16, True, seed=7)
+    cfg = B.ba_config(8, 2, 128, 0, 1e4, 0.0, 0)
+    c = R.Context(8, 2, 128, 1e4, max_blocks=64, max_q_rows=64, workspace_bytes=b.room(cfg) + (1 << 20))
+    k, cu, delta = bf16(90, 2, 128, seed=1), ints([0, 40, 90]), ints([0, 40])
+    want, got = torch.empty_like(k), torch.zeros_like(k)
+    B.ba_reencode_k(c.ctx, k, None, 90, want, cu, delta, 2, 90)
+    B.ba_reencode_k_deferred(c.ctx, k, None, 90, got, cu, delta, 2, 90)
+    o, lse = torch.empty(4, 8, 128, device="cuda"), torch.empty(4, 8, device="cuda")
+    b.call(c, o, lse, B.BA_OUT_F32)
+    w, x, dq, dw = bf16(128, seed=2), bf16(4, 8, 128, seed=3), torch.empty(4, 8, 128, device="cuda"), torch.empty(128, device="cuda")
+    B.ba_qk_norm_rope_bwd(c.ctx, x, None, 4, None, w, None, 1e-6, o, None, dq, None, dw, None, B.BA_OUT_F32)
+    torch.cuda.synchronize()
+    assert (got == 0).all()
+    B.ba_flush(c.ctx)
+    assert torch.equal(got, want) and c.device_status() == B.BA_OK
+    check_attention(b, o, lse, B.BA_OUT_F32, 128 ** -0.5)
+    c.close()
+
+
 def test_the_calls_without_the_extension(monkeypatch):
     """Through ctypes: the same bits as through the extension."""
     shape = (6, 2, 64)
