@@ -388,6 +388,8 @@ def _rows(t, what: str):
         return t.data_ptr(), 0
     if t.dim() != 3 or t.stride(2) != 1 or t.stride(1) != t.shape[2]:
         raise ValueError(f"{what}: the heads of a row must lie side by side")
+    if t.stride(0) < t.shape[1] * t.shape[2]:                  # (an expanded row's stride, 0, would say that rows are packed)
+        raise ValueError(f"{what}: rows must lie apart, a whole row or more")
     return t.data_ptr(), t.stride(0)
 
 

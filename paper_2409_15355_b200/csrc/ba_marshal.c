@@ -78,7 +78,8 @@ static int to_size(PyObject *o, size_t *out) {
   *out = PyLong_AsSize_t(o);
   return *out == (size_t)-1 && PyErr_Occurred() ? unusual_if(PyExc_OverflowError) : 1;
 }
-/* A [rows, heads, head_dim] tensor whose rows may lie apart: its data and row stride (0: packed).  Anything else is the other way's. */
+/* A [rows, heads, head_dim] tensor whose rows may lie apart, a whole row or more: its data and row stride (0: packed).  Anything else -- rows that
+ * share memory, whose stride would be taken for packed rows -- is the other way's. */
 static int to_rows(PyObject *o, void **out, int64_t *stride) {
   *stride = 0;
   if (o == Py_None || PyLong_Check(o)) return to_address(o, out);
@@ -92,7 +93,8 @@ static int to_rows(PyObject *o, void **out, int64_t *stride) {
     int k = UNUSUAL;
     if (st && sh && PyTuple_Check(st) && PyTuple_Check(sh) && PyTuple_GET_SIZE(st) == 3 && PyTuple_GET_SIZE(sh) == 3) {
       const long long s0 = PyLong_AsLongLong(PyTuple_GET_ITEM(st, 0)), s1 = PyLong_AsLongLong(PyTuple_GET_ITEM(st, 1));
-      if (PyLong_AsLongLong(PyTuple_GET_ITEM(st, 2)) == 1 && s1 == PyLong_AsLongLong(PyTuple_GET_ITEM(sh, 2)) && !PyErr_Occurred()) { *stride = s0; k = 1; }
+      const long long heads = PyLong_AsLongLong(PyTuple_GET_ITEM(sh, 1)), d = PyLong_AsLongLong(PyTuple_GET_ITEM(sh, 2));
+      if (PyLong_AsLongLong(PyTuple_GET_ITEM(st, 2)) == 1 && s1 == d && d > 0 && s0 / d >= heads && !PyErr_Occurred()) { *stride = s0; k = 1; }
     }
     Py_XDECREF(st); Py_XDECREF(sh);
     PyErr_Clear();
