@@ -459,8 +459,8 @@ ba_status ba_qk_norm_rope_bwd(ba_ctx *ctx, const void *q, int64_t q_stride, cons
  *   seq_start    device int32 [n_seqs]: the place in list s of pages that the sequence's first row goes to (its rows so far)
  *   pages        lists page_cu[s] .. of the sequences in the pools (ba_page_table, with sequences for blocks)
  *   k_pool, v_pool  bf16 [n_pages * page_rows, n_kv_heads, head_dim]; q, k, v do not overlap them
- * A row whose place has no page in its list, or a page outside the pool, is not written to the pools and reported through
- * ba_last_device_status() as BA_ERR_INVALID_ARG; its query is still written.  Two rows must not go to the same place.
+ * A row whose place has no page in its list (a list with page_cu[s] below zero has none), or a page outside the pool, is not written to
+ * the pools and reported through ba_last_device_status() as BA_ERR_INVALID_ARG; its query is still written.  Two rows must not go to the same place.
  */
 ba_status ba_append_paged(ba_ctx *ctx, const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
                           int32_t n_rows, const int32_t *pos, const void *w_q, const void *w_k, float eps, const int32_t *seq_cu,
@@ -493,8 +493,8 @@ typedef struct {
  *   o            [n_q_rows, n_q_heads, head_dim] bf16 or fp32, apart from every input; lse fp32 [n_q_rows, n_q_heads] or NULL
  * What lies behind the end of a prefix, a sequence or a list in pages or rows is never used and may hold any bits.  A page number outside
  * its pool counts as zeros and is reported (BA_ERR_INVALID_ARG).  Tables that do not fit together (a cumulative table that decreases
- * or leaves its range, a length below zero or above its list's pages) are reported the same way and nothing is written; so is an
- * amount of work beyond any launch (key tiles of 128 x KV heads x 256 query rows of all entries above six hundred million).
+ * or leaves its range, a list of pages that begins below zero, a length below zero or above its list's pages) are reported the same way
+ * and nothing is written; so is an amount of work beyond any launch (key tiles of 128 x KV heads x 256 query rows of all entries above six hundred million).
  * Uses ba_shared_prefix_bytes() bytes of workspace at most (to be given to ba_create(); BA_ERR_WORKSPACE otherwise); batch + n_groups is
  * at most BA_SHARED_MAX (BA_ERR_UNSUPPORTED).  No atomics: results are run-to-run identical.
  */

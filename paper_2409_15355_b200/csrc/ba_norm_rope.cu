@@ -228,7 +228,8 @@ struct AppendWalk {
       }
       if (!query) {
         start = __ldg(p.seq_start + s);
-        list = __ldg(p.page_cu + s); n_list = __ldg(p.page_cu + s + 1) - list;
+        list = __ldg(p.page_cu + s);
+        n_list = list >= 0 ? __ldg(p.page_cu + s + 1) - list : 0;      // (a list that begins before the table has no pages)
       }
     }
     if (query) return row;

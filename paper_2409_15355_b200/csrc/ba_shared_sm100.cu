@@ -135,14 +135,14 @@ __device__ __forceinline__ bool load_entry(const SharedParams &p, int e, Entry &
   int a, b;
   if (e < p.n_groups) {
     a = p.group_cu ? __ldg(p.group_cu + e) : 0; b = p.group_cu ? __ldg(p.group_cu + e + 1) : p.batch;
-    const int r0 = __ldg(p.prefix_cu + e), r1 = __ldg(p.prefix_cu + e + 1);
-    const long long room = p.prefix_paged ? ((long long)__ldg(p.prefix_page_cu + e + 1) - __ldg(p.prefix_page_cu + e)) << p.prefix_page_lg : p.n_prefix_rows - r0;
-    if (a < 0 || b < a || b > p.batch || r0 < 0 || r1 < r0 || r1 - r0 > room) return false;
+    const int r0 = __ldg(p.prefix_cu + e), r1 = __ldg(p.prefix_cu + e + 1), list = p.prefix_paged ? __ldg(p.prefix_page_cu + e) : 0;
+    const long long room = p.prefix_paged ? ((long long)__ldg(p.prefix_page_cu + e + 1) - list) << p.prefix_page_lg : (long long)p.n_prefix_rows - r0;
+    if (a < 0 || b < a || b > p.batch || r0 < 0 || r1 < r0 || list < 0 || r1 - r0 > room) return false;
     x.len = r1 - r0;
   } else {
-    const int s = e - p.n_groups, len = __ldg(p.own_len + s);
-    const long long room = ((long long)__ldg(p.page_cu + s + 1) - __ldg(p.page_cu + s)) << p.page_lg;
-    if (len < 0 || len > room) return false;
+    const int s = e - p.n_groups, len = __ldg(p.own_len + s), list = __ldg(p.page_cu + s);
+    const long long room = ((long long)__ldg(p.page_cu + s + 1) - list) << p.page_lg;
+    if (len < 0 || list < 0 || len > room) return false;
     a = s; b = s + 1; x.len = len;
   }
   const int first = q_begin(p, a), last = q_begin(p, b);   // (their difference may not fit where they do not hold)
