@@ -495,6 +495,9 @@ typedef struct {
  * its pool counts as zeros and is reported (BA_ERR_INVALID_ARG).  Tables that do not fit together (a cumulative table that decreases
  * or leaves its range, a list of pages that begins below zero, a length below zero or above its list's pages) are reported the same way
  * and nothing is written; so is an amount of work beyond any launch (key tiles of 128 x KV heads x 256 query rows of all entries above six hundred million).
+ * Keys, values and queries that are not finite act as in the formula: a row that sees a score which is NaN or +infinity is NaN, and so is its
+ * log-sum-exp; a value that is NaN makes its column NaN.  (A value counts, with weight zero, for the rows of its sequence that come before
+ * it as well: zero times NaN.  A key does not.)
  * Uses ba_shared_prefix_bytes() bytes of workspace at most (to be given to ba_create(); BA_ERR_WORKSPACE otherwise); batch + n_groups is
  * at most BA_SHARED_MAX (BA_ERR_UNSUPPORTED).  No atomics: results are run-to-run identical.
  */

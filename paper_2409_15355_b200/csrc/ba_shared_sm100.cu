@@ -26,6 +26,9 @@
 // 16 sequences of one token over a prefix of 32000 keys 36 us (20 of them the prefix's bytes); 24 questions of 17-64 tokens over 16384 keys 280 us,
 // 50 % of the tensor pipe: a pair of tiles takes 3270 cycles, its products 2100, the chain from scores over softmax to scores is what is left.
 //
+// A score that is NaN or +infinity leaves a NaN in its row's sum (the maximum does not show it), as in the formula.  So a sum of zero is what
+// marks a row that saw no key; any other is divided by, and a NaN goes through to o and lse whatever the cuts.
+//
 // Rounding: P to bf16 (the products' type; 2^-8 relative at most, the sums of the softmax are taken before it), o once at the end.
 #include <algorithm>
 
@@ -455,11 +458,11 @@ __device__ __forceinline__ void consume_run(const SharedParams &p, FewRun run, u
 #pragma unroll
       for (int w = 0; w < kWarps; ++w) {
         const float2 v = stat[w * kRows + r];
-        if (v.x != -INFINITY) den += v.y * ex2((v.x - top) * sl);
+        if (v.y != 0.f) den += v.y * ex2((v.x - top) * sl);
       }
-      f[hi] = mx[hi] != -INFINITY && den > 0.f ? ex2((mx[hi] - top) * sl) / den : 0.f;
+      f[hi] = sum[hi] != 0.f ? ex2((mx[hi] - top) * sl) / den : 0.f;
       if (ok && warp == 0 && in_quad == 0 && r < n_rows) {
-        const float lse = den > 0.f ? (top * sl + log2f(den)) * 0.6931471805599453f : -INFINITY;
+        const float lse = den != 0.f ? (top * sl + log2f(den)) * 0.6931471805599453f : -INFINITY;
         if (!direct) p.part[p.n_part * D + place(r)] = lse;
         else if (p.lse) p.lse[place(r)] = lse;
       }
@@ -852,10 +855,10 @@ __device__ __forceinline__ void many_rows(const SharedParams &p, const CUtensorM
       const RowMap map(p, k.x, k.row0, k.head);
       const long long base = k.tile0 == 0 ? first_part(p, (own ? 0 : 1) + (pair ? 0 : 2 * t)) : cut_part(p, (int)blockIdx.x) + (pair ? 0 : t * 128);
       auto place = [&](int rr) { return base + (k.tile0 == 0 ? map.row(rr) : rr); };
-      const float lse = l > 0.f ? (m_used * sl + log2f(l)) * 0.6931471805599453f : -INFINITY;
+      const float lse = l != 0.f ? (m_used * sl + log2f(l)) * 0.6931471805599453f : -INFINITY;
       if (row < k.n_rows) p.part[p.n_part * D + place(row)] = lse;
       if (j0 >= k.n) continue;                             // (no tile for this group)
-      const float inv = l > 0.f ? 1.f / l : 0.f;
+      const float inv = l != 0.f ? 1.f / l : 0.f;
       ok = __all_sync(0xffffffffu, mbar_wait(&ctrl->o_done[t], o_uses & 1, abort_flag));
       ++o_uses;
       if (!ok) break;
@@ -1074,32 +1077,34 @@ ba_shared_merge_kernel(const __grid_constant__ SharedParams p, int warps_a_row) 
   const int rounds = __reduce_max_sync(0xffffffffu, i_end - i_begin);
   for (int i0 = 0; i0 < rounds; i0 += kL) {
     const int i = i_begin + i0 + lane;
-    long long at = 0;
+    long long at = -1;                                     // (of an empty result: it holds no values at all)
     float lse = -INFINITY;
     if (i < i_end) {
       const int side = i >= n[0], k = i - (side ? n[0] : 0), two = (side ? per[1] : per[0]) - 1, piece = k >> two, second = k & two;
       at = piece == 0 ? first_part(p, (side ? 0 : 1) + 2 * second) + here
                       : cut_part(p, (side ? c0[1] : c0[0]) + piece) + (side ? tile_row[1] : tile_row[0]) + 128 * second;
       lse = p.part[p.n_part * D + at];
+      if (lse == -INFINITY) at = -1;
     }
     float mx = fmaxf(lse, top);
 #pragma unroll
     for (int d = kL / 2; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
-    const float w = lse == -INFINITY ? 0.f : __expf(lse - mx);
+    const float w = at < 0 ? 0.f : __expf(lse - mx);       // (a NaN stays one)
     rescale(mx);
     for (int k0 = 0; k0 < min(kL, rounds - i0); k0 += kBatch) {
       float wk[kBatch], f[kBatch][kV];
 #pragma unroll
       for (int k = 0; k < kBatch; ++k) {
         wk[k] = __shfl_sync(0xffffffffu, w, (k0 + k) & (kL - 1), kL);          // (kL is a multiple of kBatch)
-        const float *x = p.part + __shfl_sync(0xffffffffu, at, (k0 + k) & (kL - 1), kL) * D + lane * kVec;
+        const long long from = __shfl_sync(0xffffffffu, at, (k0 + k) & (kL - 1), kL);
+        const float *x = p.part + from * D + lane * kVec;
 #pragma unroll
-        for (int c = 0; c < kChunks; ++c) {                // (an empty result holds no values at all)
+        for (int c = 0; c < kChunks; ++c) {
           if (kVec == 4) {
-            const float4 v = wk[k] == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : __ldcs(reinterpret_cast<const float4 *>(x + c * kL * kVec));
+            const float4 v = from < 0 ? make_float4(0.f, 0.f, 0.f, 0.f) : __ldcs(reinterpret_cast<const float4 *>(x + c * kL * kVec));
             f[k][c * kVec] = v.x; f[k][c * kVec + 1] = v.y; f[k][c * kVec + 2 % kVec] = v.z; f[k][c * kVec + 3 % kVec] = v.w;
           } else {
-            const float2 v = wk[k] == 0.f ? make_float2(0.f, 0.f) : __ldcs(reinterpret_cast<const float2 *>(x + c * kL * kVec));
+            const float2 v = from < 0 ? make_float2(0.f, 0.f) : __ldcs(reinterpret_cast<const float2 *>(x + c * kL * kVec));
             f[k][c * kVec] = v.x; f[k][c * kVec + 1] = v.y;
           }
         }
@@ -1122,7 +1127,7 @@ ba_shared_merge_kernel(const __grid_constant__ SharedParams p, int warps_a_row) 
     if (share > 0) return;
     for (int k = 1; k < warps_a_row; ++k) {
       const float t = others[warp + k][32 * kV], d = others[warp + k][32 * kV + 1];
-      if (t == -INFINITY) continue;
+      if (d == 0.f) continue;
       rescale(fmaxf(top, t));
       const float f = __expf(t - top);
       den = fmaf(d, f, den);
@@ -1131,7 +1136,7 @@ ba_shared_merge_kernel(const __grid_constant__ SharedParams p, int warps_a_row) 
     }
   }
   if (!needed) return;
-  const float inv = den > 0.f ? 1.f / den : 0.f;
+  const float inv = den != 0.f ? 1.f / den : 0.f;
 #pragma unroll
   for (int v = 0; v < kV; ++v) acc[v] *= inv;
 #pragma unroll
@@ -1148,7 +1153,7 @@ ba_shared_merge_kernel(const __grid_constant__ SharedParams p, int warps_a_row) 
       else *reinterpret_cast<uint32_t *>(o) = pack_bf16(a[0], a[1]);
     }
   }
-  if (p.lse && lane == 0) p.lse[here] = den > 0.f ? top + logf(den) : -INFINITY;
+  if (p.lse && lane == 0) p.lse[here] = den != 0.f ? top + logf(den) : -INFINITY;
 }
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }

@@ -59,3 +59,47 @@ def test_attention_over_a_list_that_begins_before_the_table(which):
     assert c.device_status() == B.BA_OK
     check_attention(b, o, lse, B.BA_OUT_F32, 0.125)
     c.close()
+
+
+# ------------------------------------------------------------------ values that are not finite
+QUESTIONS = {"few rows": [1, 2, 1], "a query tile": [20, 1, 10], "two query tiles": [70, 40, 3]}
+PLANTED = [("key of the prefix", float("nan")), ("key of the prefix", float("inf")), ("key of the prefix", float("-inf")), ("every key of the prefix", float("nan")),
+           ("last key of its own", float("nan")), ("last key of its own", float("inf")), ("key of a sequence alone", float("nan")),
+           ("key of a sequence alone", float("inf")), ("query", float("nan")), ("query", float("inf")), ("value of the prefix", float("nan"))]
+
+
+@pytest.mark.parametrize("shape", [(4, 2, 64), (8, 2, 128)], ids=str)
+@pytest.mark.parametrize("questions", list(QUESTIONS))
+@pytest.mark.parametrize("alone", [100, 4000], ids=["whole", "cut"])
+@pytest.mark.parametrize("where,value", PLANTED, ids=str)
+def test_values_that_are_not_finite_go_through(shape, questions, alone, where, value):
+    """As in the formula: a row that sees a score which is NaN or +infinity is NaN, its log-sum-exp too, wherever the work is cut; every other
+    row is what it would be."""
+    q_lens = QUESTIONS[questions]
+    b = Batch(shape, [2000], [0, 3], q_lens + [1], [300, 40, 5, alone], 16, False, seed=11)
+    own = [tk.page_rows_of(b.cu, b.idx, 16, s, n) for s, n in enumerate(b.own)]
+    if where == "key of the prefix":
+        b.kv_prefix[0][b.prefix_rows[0][1333], 1, 5] = value
+    elif where == "every key of the prefix":
+        b.kv_prefix[0][b.prefix_rows[0], 1, 5] = value
+    elif where == "last key of its own":
+        b.pool[0][own[0][-1], 1, 5] = value
+    elif where == "key of a sequence alone":
+        b.pool[0][own[3][alone // 2], 1, 5] = value
+    elif where == "query":
+        b.q[sum(q_lens[:2]), 1, 5] = value                      # (its scores are infinite with either sign, and NaN without)
+    else:
+        b.kv_prefix[1][b.prefix_rows[0][1333], 1, 5] = value
+    c = make_context(shape, b)
+    o, lse = torch.full((b.rows, *shape[::2]), 5.0, device="cuda"), torch.full((b.rows, shape[0]), 6.0, device="cuda")
+    b.call(c, o, lse, B.BA_OUT_F32)
+    assert c.device_status() == B.BA_OK
+    with np.errstate(all="ignore"):
+        want, want_lse, size = b.reference(shape[2] ** -0.5)
+    got, got_lse, fine = f64(o), f64(lse), np.isfinite(want)
+    assert (np.isnan(got) == ~fine).all() and (np.isnan(got_lse) == np.isnan(want_lse)).all()
+    assert fine.any() and (np.isinf(value) or not fine.all())       # (an infinite key's scores are infinite with the query's sign)
+    assert (np.abs(got - want)[fine] <= (HALF_STEP + 1e-4) * size[fine]).all()
+    known = ~np.isnan(want_lse)
+    assert (np.abs(got_lse - want_lse)[known] <= 1e-4).all()
+    c.close()
