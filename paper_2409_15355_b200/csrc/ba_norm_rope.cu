@@ -11,6 +11,9 @@
 // pairs a lane into the weights and walks the heads; with few rows the heads of a row are shared out among warps instead.  The values
 // of two rotary pairs are kept side by side, first members and second members, for arithmetic on two floats at a time.
 //
+// Kernels are launched early (ba_pdl_wait), so that tables, positions and sums may be written by the kernel before while one is alive already:
+// they are read by plain loads, not through the read-only path, which wants data that nobody writes in a kernel's lifetime.
+//
 // Measured, heads of 128: 131072 rows of 32 + 8 heads 476 us (5.65 TB/s, 86 % of a copy), their gradients at 32768 rows 190 us (5.3 TB/s) and
 // 5 us for the weights' sums; 64 passages of 1000 rows into pages 109 us (4.8 TB/s); one row each of 16 sequences 4 us.
 #include <string.h>
@@ -219,24 +222,24 @@ struct AppendWalk {
       page_at = -1;
       if (p.seq_cu) {
         int lo = 0, hi = p.n_seqs + 1;                     // first index whose start lies behind the row
-        while (lo < hi) { const int mid = (lo + hi) >> 1; if (__ldg(p.seq_cu + mid) <= row) lo = mid + 1; else hi = mid; }
+        while (lo < hi) { const int mid = (lo + hi) >> 1; if (p.seq_cu[mid] <= row) lo = mid + 1; else hi = mid; }
         s = lo - 1;
         if (s < 0 || s >= p.n_seqs) { s = -1; return -2; }
-        first = __ldg(p.seq_cu + s); end = __ldg(p.seq_cu + s + 1);
+        first = p.seq_cu[s]; end = p.seq_cu[s + 1];
       } else {
         s = first = row; end = row + 1;
       }
       if (!query) {
-        start = __ldg(p.seq_start + s);
-        list = __ldg(p.page_cu + s);
-        n_list = list >= 0 ? __ldg(p.page_cu + s + 1) - list : 0;      // (a list that begins before the table has no pages)
+        start = p.seq_start[s];
+        list = p.page_cu[s];
+        n_list = list >= 0 ? p.page_cu[s + 1] - list : 0;    // (a list that begins before the table has no pages)
       }
     }
     if (query) return row;
     const long long place = start + (row - first), nth = place >> p.page_lg;
     if (nth != page_at || page_at < 0) {
       page_at = nth;
-      const int page = nth >= 0 && nth < n_list ? __ldg(p.page_idx + list + nth) : -1;
+      const int page = nth >= 0 && nth < n_list ? p.page_idx[list + nth] : -1;
       page_row = page >= 0 && page < p.n_pages ? (long long)page << p.page_lg : -1;
     }
     if (page_row < 0) {
@@ -290,7 +293,7 @@ ba_norm_rope_kernel(const __grid_constant__ NormParams p) {
     for (int row = un.row; row < un.row_end; ++row) {
       const __nv_bfloat16 *src = side.x + row * side.stride + sub * D;
       long long to = row;
-      const int pos = p.pos ? __ldg(p.pos + row) : 0;
+      const int pos = p.pos ? p.pos[row] : 0;
       Eight wc, ws;                        // weights x cos, weights x sin
       for (int i0 = begin; i0 < end; i0 += kAhead) {
         Raw16 raw[kAhead];
@@ -362,7 +365,7 @@ ba_norm_rope_bwd_kernel(const __grid_constant__ NormParams p) {
     const NormUnit un = unit_at(side, p.n_rows, steps, u);
     const int begin = un.step, end = un.step_end;
     for (int row = un.row; row < un.row_end; ++row) {
-      const int pos = p.pos ? __ldg(p.pos + row) : 0;
+      const int pos = p.pos ? p.pos[row] : 0;
       const __nv_bfloat16 *src = side.x + row * side.stride + sub * D;
       const T *dy = reinterpret_cast<const T *>(side.dy) + ((long long)row * side.heads + sub) * D;
       T *dx = reinterpret_cast<T *>(side.y) + row * side.y_stride + sub * D;
@@ -444,7 +447,7 @@ ba_norm_dw_kernel(const float *part, int n_q, int n_k, float *dw_q, float *dw_k)
   if (!dw) return;
   float t = 0.f;
 #pragma unroll 4
-  for (int b = run; b < n; b += 32) t += __ldg(part + (size_t)(first + b) * D + col);
+  for (int b = run; b < n; b += 32) t += part[(size_t)(first + b) * D + col];
   sums[run][threadIdx.x & 31] = t;
   __syncthreads();
   t = sums[threadIdx.x & 31][run];                         // (column `run` of the 32, a run of CTAs a lane)

@@ -116,19 +116,21 @@ struct SharedCtrl {
 };
 static_assert(sizeof(SharedCtrl) <= kCtrlBytes, "control area");
 
+// Tables and queries may come from the kernel before (ba_segment, ba_append_paged), beside which this one is launched: plain loads throughout, as the
+// read-only path wants data that nobody writes in a kernel's lifetime.
 // An entry, looked up by the thread that asks: rows q_row0 .. of the queries, `len` keys.
 struct Entry { int q_row0, rows, len; };
-__device__ __forceinline__ int q_begin(const SharedParams &p, int s) { return p.q_cu ? __ldg(p.q_cu + s) : s; }
+__device__ __forceinline__ int q_begin(const SharedParams &p, int s) { return p.q_cu ? p.q_cu[s] : s; }
 __device__ __forceinline__ Entry get_entry(const SharedParams &p, int e) {
   Entry x;
   if (e < p.n_groups) {
-    const int a = p.group_cu ? __ldg(p.group_cu + e) : 0, b = p.group_cu ? __ldg(p.group_cu + e + 1) : p.batch;
+    const int a = p.group_cu ? p.group_cu[e] : 0, b = p.group_cu ? p.group_cu[e + 1] : p.batch;
     x.q_row0 = q_begin(p, a); x.rows = q_begin(p, b) - x.q_row0;
-    x.len = __ldg(p.prefix_cu + e + 1) - __ldg(p.prefix_cu + e);
+    x.len = p.prefix_cu[e + 1] - p.prefix_cu[e];
   } else {
     const int s = e - p.n_groups;
     x.q_row0 = q_begin(p, s); x.rows = q_begin(p, s + 1) - x.q_row0;
-    x.len = __ldg(p.own_len + s);
+    x.len = p.own_len[s];
   }
   return x;
 }
@@ -137,14 +139,14 @@ __device__ __forceinline__ bool load_entry(const SharedParams &p, int e, Entry &
   x.q_row0 = x.rows = x.len = 0;
   int a, b;
   if (e < p.n_groups) {
-    a = p.group_cu ? __ldg(p.group_cu + e) : 0; b = p.group_cu ? __ldg(p.group_cu + e + 1) : p.batch;
-    const int r0 = __ldg(p.prefix_cu + e), r1 = __ldg(p.prefix_cu + e + 1), list = p.prefix_paged ? __ldg(p.prefix_page_cu + e) : 0;
-    const long long room = p.prefix_paged ? ((long long)__ldg(p.prefix_page_cu + e + 1) - list) << p.prefix_page_lg : (long long)p.n_prefix_rows - r0;
+    a = p.group_cu ? p.group_cu[e] : 0; b = p.group_cu ? p.group_cu[e + 1] : p.batch;
+    const int r0 = p.prefix_cu[e], r1 = p.prefix_cu[e + 1], list = p.prefix_paged ? p.prefix_page_cu[e] : 0;
+    const long long room = p.prefix_paged ? ((long long)p.prefix_page_cu[e + 1] - list) << p.prefix_page_lg : (long long)p.n_prefix_rows - r0;
     if (a < 0 || b < a || b > p.batch || r0 < 0 || r1 < r0 || list < 0 || r1 - r0 > room) return false;
     x.len = r1 - r0;
   } else {
-    const int s = e - p.n_groups, len = __ldg(p.own_len + s), list = __ldg(p.page_cu + s);
-    const long long room = ((long long)__ldg(p.page_cu + s + 1) - list) << p.page_lg;
+    const int s = e - p.n_groups, len = p.own_len[s], list = p.page_cu[s];
+    const long long room = ((long long)p.page_cu[s + 1] - list) << p.page_lg;
     if (len < 0 || list < 0 || len > room) return false;
     a = s; b = s + 1; x.len = len;
   }
@@ -199,7 +201,7 @@ __device__ __forceinline__ int group_of(const SharedParams &p, int s) {
   if (p.n_groups == 0) return -1;
   if (!p.group_cu) return 0;
   int lo = 0, hi = p.n_groups + 1;
-  while (lo < hi) { const int mid = (lo + hi) >> 1; if (__ldg(p.group_cu + mid) <= s) lo = mid + 1; else hi = mid; }
+  while (lo < hi) { const int mid = (lo + hi) >> 1; if (p.group_cu[mid] <= s) lo = mid + 1; else hi = mid; }
   return lo - 1 < p.n_groups ? lo - 1 : -1;
 }
 
@@ -239,9 +241,9 @@ __device__ __forceinline__ Source source_of(const SharedParams &p, const Piece &
   s.paged = own || p.prefix_paged;
   s.lg = own ? p.page_lg : p.prefix_page_lg; s.n_pages = own ? p.n_pages : p.prefix_pages;
   s.sub_rows = s.paged ? min(kTile, 1 << s.lg) : kTile;
-  s.list = own ? __ldg(p.page_cu + k.e - p.n_groups) : s.paged ? __ldg(p.prefix_page_cu + k.e) : 0;
+  s.list = own ? p.page_cu[k.e - p.n_groups] : s.paged ? p.prefix_page_cu[k.e] : 0;
   s.idx = own ? p.page_idx : p.prefix_page_idx;
-  s.first = s.paged ? 0 : __ldg(p.prefix_cu + k.e);
+  s.first = s.paged ? 0 : p.prefix_cu[k.e];
   s.len = k.x.len;
   return s;
 }
@@ -250,7 +252,7 @@ __device__ __forceinline__ int box_row(const SharedParams &p, const Source &s, i
   const int lane = threadIdx.x & 31, t = tile * kTile + lane * s.sub_rows;
   if (lane * s.sub_rows >= kTile || t >= s.len) return -1;
   if (!s.paged) return s.first + t;
-  const int page = __ldg(s.idx + s.list + (t >> s.lg));
+  const int page = s.idx[s.list + (t >> s.lg)];
   if (page < 0 || page >= s.n_pages) {
     ba_record_status(p.status, BA_ERR_INVALID_ARG);
     return s.n_pages << s.lg;                              // behind the pool: the copy engine fills in zeros
@@ -301,8 +303,8 @@ __device__ __forceinline__ void load_queries(const SharedParams &p, const Piece 
     limit[hi] = own ? k.x.len - (k.x.rows - 1 - map.token(there ? r : 0)) : k.x.len;
 #pragma unroll
     for (int c = 0; c < D / 16; ++c) {
-      qa[c][hi] = there ? __ldg(src + c * 8) : 0u;
-      qa[c][hi + 2] = there ? __ldg(src + c * 8 + 4) : 0u;
+      qa[c][hi] = there ? src[c * 8] : 0u;
+      qa[c][hi + 2] = there ? src[c * 8 + 4] : 0u;
     }
   }
 }
@@ -938,7 +940,7 @@ ba_shared_attend_kernel(const __grid_constant__ CUtensorMap tmap_kx, const __gri
     sum[is_many(p, one)] += lay_of(p, one).a_head() * p.Hkv;
     if (one.rows * p.G > 128) atomicOr(&ctrl->pairs[e >> 5], 1u << (e & 31));
     if (e < p.n_groups && one.len > 0) {                   // its sequences do not write their rows straight to the output
-      const int a = p.group_cu ? __ldg(p.group_cu + e) : 0, b = p.group_cu ? __ldg(p.group_cu + e + 1) : p.batch;
+      const int a = p.group_cu ? p.group_cu[e] : 0, b = p.group_cu ? p.group_cu[e + 1] : p.batch;
       for (int w = a >> 5; w <= (b - 1) >> 5 && a < b; ++w) {
         const unsigned from = w == a >> 5 ? ~0u << (a & 31) : ~0u, to = w == (b - 1) >> 5 ? ~0u >> (31 - ((b - 1) & 31)) : ~0u;
         atomicOr(&ctrl->prefixed[w], from & to);
@@ -1023,7 +1025,7 @@ ba_shared_merge_kernel(const __grid_constant__ SharedParams p, int warps_a_row) 
   int s = row, g = -1, row0[2] = {0, 0};
   if (there && p.q_cu) {
     int lo = 0, hi = p.batch + 1;
-    while (lo < hi) { const int mid = (lo + hi) >> 1; if (__ldg(p.q_cu + mid) <= row) lo = mid + 1; else hi = mid; }
+    while (lo < hi) { const int mid = (lo + hi) >> 1; if (p.q_cu[mid] <= row) lo = mid + 1; else hi = mid; }
     s = lo - 1;
   }
   // (lanes whose row is not there or complete go on without results: the warps of a CTA meet)
@@ -1031,7 +1033,7 @@ ba_shared_merge_kernel(const __grid_constant__ SharedParams p, int warps_a_row) 
   if (needed) {
     g = group_of(p, s);
     row0[1] = q_begin(p, s);
-    if (g >= 0 && p.group_cu) { const int a = __ldg(p.group_cu + g); row0[0] = a >= 0 && a <= p.batch ? q_begin(p, a) : 0; }    // (not checked yet)
+    if (g >= 0 && p.group_cu) { const int a = p.group_cu[g]; row0[0] = a >= 0 && a <= p.batch ? q_begin(p, a) : 0; }    // (not checked yet)
     else if (g >= 0) row0[0] = q_begin(p, 0);
   }
   ba_pdl_wait();

@@ -103,3 +103,56 @@ def test_values_that_are_not_finite_go_through(shape, questions, alone, where, v
     known = ~np.isnan(want_lse)
     assert (np.abs(got_lse - want_lse)[known] <= 1e-4).all()
     c.close()
+
+
+# ------------------------------------------------------------------ calls that follow one another closely
+def test_results_of_calls_in_close_succession():
+    """Nothing waits between the calls, and each reads what the one before has just written: the weights' sums out of the workspace, queries and
+    keys out of the append, positions and lengths out of the tables' call.  Every round gives what it gives alone."""
+    shape = (8, 2, 64)
+    hq, hkv, d = shape
+    lens = [[40, 17, 1], [9, 70, 1], [3, 2, 1]]
+    n = 40
+    cfg = B.ba_config(*shape, 0, 1e4, 0.0, 0)
+    c = R.Context(*shape, 1e4, max_blocks=64, max_q_rows=256, workspace_bytes=B.ba_shared_prefix_bytes(cfg, n, 1, n))
+    w = bf16(d, seed=1)
+    prefix = [bf16(200, hkv, d, seed=s) for s in (2, 3)]
+    page_cu, page_idx, start, own = ints(range(n + 1)), ints(reversed(range(n))), ints([0] * n), ints([1] * n)
+    table = B.make_page_table(16, n, page_cu, page_idx)
+    pools = [torch.zeros(n * 16, hkv, d, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    segments = [np.asarray(x, dtype=np.int32) for x in lens]
+    buf = torch.empty(B.ba_segments_bytes(1, 3, 80), dtype=torch.uint8, device="cuda")
+    q_out = torch.empty(n, hq, d, dtype=torch.bfloat16, device="cuda")
+
+    def round_(k, out):
+        x = inputs[k]
+        rows = int(segments[k].sum())
+        seg = B.ba_segment(c.ctx, segments[k], np.asarray([3], dtype=np.int32), 1, 3, rows, B.BA_MODE_BLOCK, buf)
+        B.ba_qk_norm_rope(c.ctx, x[:rows, :hq], None, rows, seg.tok_pos, w, None, 1e-6, out["q"][:rows], None)
+        B.ba_qk_norm_rope_bwd(c.ctx, x[:rows, :hq], None, rows, seg.tok_pos, w, None, 1e-6, out["q"][:rows], None, out["dq"][:rows], None, out["dw"], None,
+                              B.BA_OUT_BF16)
+        B.ba_append_paged(c.ctx, x[:n, :hq], x[:n, hq:hq + hkv], x[:n, hq + hkv:], n, start, w, w, 1e-6, None, start, n, q_out, *pools, table)
+        shared = B.make_shared_batch(n, 1, None, seg.cu_cache_seq, None, own)           # (the prefix: the cached tokens of the tables)
+        B.ba_shared_prefix_attend(c.ctx, q_out, n, *prefix, 200, None, *pools, table, shared, out["o"], out["lse"], B.BA_OUT_F32)
+
+    inputs = [bf16(80, hq + 2 * hkv, d, seed=20 + k) for k in range(3)]
+    room = lambda: {"q": torch.zeros(80, hq, d, dtype=torch.bfloat16, device="cuda"), "dq": torch.zeros(80, hq, d, dtype=torch.bfloat16, device="cuda"),
+                    "dw": torch.zeros(d, device="cuda"), "o": torch.zeros(n, hq, d, device="cuda"), "lse": torch.zeros(n, hq, device="cuda")}
+    alone = []
+    for k in range(3):
+        alone.append(room())
+        torch.cuda.synchronize()
+        round_(k, alone[k])
+        torch.cuda.synchronize()
+    outs = [room() for _ in range(30)]
+    torch.cuda.synchronize()
+    for i, out in enumerate(outs):
+        round_(i % 3, out)
+    torch.cuda.synchronize()
+    assert c.device_status() == B.BA_OK
+    for i, out in enumerate(outs):
+        for key, want in alone[i % 3].items():
+            assert torch.equal(out[key], want), (i, key)
+    for key in ("q", "o", "dw"):
+        assert not torch.equal(alone[0][key], alone[1][key])
+    c.close()
