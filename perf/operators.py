@@ -219,7 +219,6 @@ def prepare(case, seed):
         s.lse = torch.empty(rows, hq, device=DEVICE)
     if own:                                                  # the handle and the tables that a program keeps
         from paper_2409_15355_b200 import binding as B
-        from paper_2409_15355_b200 import runtime as R
         layout = B.BA_ROPE_HALF if c["rope"] == "half" else B.BA_ROPE_ADJACENT
         cfg = B.ba_config(hq, hkv, d, layout, float(c["theta"]), 0.0, 0)
         if c["op"] == "shared":
@@ -229,8 +228,18 @@ def prepare(case, seed):
             s.prefix_table = None if c["packed_prefix"] else B.make_page_table(c["page_rows"], s.prefix_pages, s.prefix_page_cu, s.prefix_page_idx)
         if c["op"] == "append":
             s.table = B.make_page_table(c["page_rows"], s.n_pages, s.page_cu, s.page_idx)
-        s.context = R.Context(hq, hkv, d, c["theta"], rope_layout=layout, max_blocks=64, max_q_rows=64, workspace_bytes=room)
+        s.context = _context(hq, hkv, d, c["theta"], layout, room)
     return s
+
+
+def _context(hq, hkv, d, theta, layout, room, kept={}):
+    """The library's handle for a configuration.  It knows nothing of the inputs, and a program makes it once: one is kept for every
+    configuration, and made anew only where a case needs a larger workspace."""
+    from paper_2409_15355_b200 import runtime as R
+    key = hq, hkv, d, theta, layout
+    if key not in kept or kept[key][0] < room:
+        kept[key] = room, R.Context(hq, hkv, d, theta, rope_layout=layout, max_blocks=64, max_q_rows=64, workspace_bytes=room)
+    return kept[key][1]
 
 
 def run(state):
