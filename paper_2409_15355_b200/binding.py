@@ -69,12 +69,17 @@ class ba_shared_batch(C.Structure):
                 ("q_cu", C.c_void_p), ("own_len", C.c_void_p)]
 
 
+def _check_table(t, what: str) -> None:
+    """A table that a kernel reads: an int32 tensor on the device, its address, or None."""
+    if t is not None and not isinstance(t, int) and (not getattr(t, "is_cuda", False) or str(t.dtype) != "torch.int32"):
+        raise ValueError(f"{what}: an int32 tensor on the device is wanted")
+
+
 def make_shared_batch(batch: int, n_groups: int, group_cu, prefix_cu, q_cu, own_len) -> "ba_shared_batch":
     """group_cu / prefix_cu / q_cu / own_len: torch int32 CUDA tensors (kept alive by the caller), their addresses, or None (see
     include/ba.h)."""
     for t in (group_cu, prefix_cu, q_cu, own_len):
-        if t is not None and not isinstance(t, int) and (not getattr(t, "is_cuda", False) or str(t.dtype) != "torch.int32"):
-            raise ValueError("the tables of a shared batch are int32 tensors on the device")
+        _check_table(t, "the tables of a shared batch")
     return ba_shared_batch(batch, n_groups, _ptr(group_cu), _ptr(prefix_cu), _ptr(q_cu), _ptr(own_len))
 
 
@@ -174,12 +179,15 @@ def _load_marshal():
 
 
 _ROWS = {"ba_qk_norm_rope": (1, 2), "ba_qk_norm_rope_bwd": (1, 2, 10, 11), "ba_append_paged": (1, 2, 3)}
+_TABLES = {"ba_qk_norm_rope": (4,), "ba_qk_norm_rope_bwd": (4,), "ba_append_paged": (5, 9, 10)}
 _MAY_BE_NULL = {("ba_shared_prefix_attend", 6)}      # structures a call can do without: packed prefixes have no pages
 
 
 def _through_ctypes(name, *args):
     """A hot call whose arguments the extension does not take: through ctypes, like every other function of the library."""
     fn = getattr(load_library(), name)
+    for i in _TABLES.get(name, ()):
+        _check_table(args[i], f"argument {i}")
     if name in _ROWS:                                          # a tensor whose rows may lie apart stands for its address and stride
         args = [x for i, a in enumerate(args) for x in (_rows(a, f"argument {i}") if i in _ROWS[name] else (a,))]
     given = [args[0]]

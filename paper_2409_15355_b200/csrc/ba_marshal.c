@@ -14,7 +14,7 @@
 
 #include "ba.h"
 
-static PyObject *s_data_ptr, *s_is_contiguous, *s_stride, *s_shape;
+static PyObject *s_data_ptr, *s_is_contiguous, *s_stride, *s_shape, *s_dtype, *s_is_cuda, *int32_type;
 static PyObject *other_way, *t_handle, *t_segments, *t_pages, *t_shared;
 /* bind()'s: the ctypes way, c_void_p, ba_segments, ba_page_table, ba_shared_batch */
 
@@ -106,6 +106,27 @@ static int to_rows(PyObject *o, void **out, int64_t *stride) {
   Py_DECREF(r);
   return k;
 }
+/* An int32 tensor on the device, by its contents' address.  Anything else -- other types, the host's -- is the other way's, which refuses it. */
+static int to_table(PyObject *o, void **out) {
+  if (o != Py_None && !PyLong_Check(o)) {
+    PyObject *t = PyObject_GetAttr(o, s_dtype);
+    if (!t) return unusual_if(PyExc_AttributeError);
+    if (!int32_type) {                             /* (torch has one object for a type; this file does not import torch) */
+      PyObject *name = PyObject_Str(t);
+      if (name && PyUnicode_Check(name) && PyUnicode_CompareWithASCIIString(name, "torch.int32") == 0) int32_type = Py_NewRef(t);
+      Py_XDECREF(name);
+      PyErr_Clear();
+    }
+    const int is = t == int32_type;
+    Py_DECREF(t);
+    PyObject *there = is ? PyObject_GetAttr(o, s_is_cuda) : NULL;
+    const int cuda = there == Py_True;
+    Py_XDECREF(there);
+    PyErr_Clear();
+    if (!cuda) return UNUSUAL;
+  }
+  return to_address(o, out);
+}
 static int to_float(PyObject *o, float *out) {
   if (!PyFloat_Check(o)) return UNUSUAL;
   *out = (float)PyFloat_AS_DOUBLE(o);
@@ -137,6 +158,7 @@ static PyObject *go_other_way(const char *name, PyObject *const *args, Py_ssize_
 #define SEG(i, v) void *v; TAKE(to_memory(args[i], t_segments, sizeof(ba_segments), &v))
 #define PAGES(i, v) void *v; TAKE(to_memory(args[i], t_pages, sizeof(ba_page_table), &v))
 #define R(i, v) void *v; int64_t v##_stride; TAKE(to_rows(args[i], &v, &v##_stride))
+#define T(i, v) void *v; TAKE(to_table(args[i], &v))
 #define F(i, v) float v; TAKE(to_float(args[i], &v))
 #define SHARED(i, v) void *v; TAKE(to_memory(args[i], t_shared, sizeof(ba_shared_batch), &v))
 #define CALL(expr)                                   \
@@ -199,18 +221,18 @@ static PyObject *m_final_attend_fused_paged(PyObject *self, PyObject *const *arg
 
 #define PRESENT(f) if (!p_##f || !t_shared) return go_other_way(function, args, nargs)
 static PyObject *m_qk_norm_rope(PyObject *self, PyObject *const *args, Py_ssize_t nargs) {
-  ARGS(ba_qk_norm_rope, 11); PRESENT(ba_qk_norm_rope); CTX; R(1, q); R(2, k); I(3, n); P(4, pos); P(5, wq); P(6, wk); F(7, eps); P(8, q_out); P(9, k_out);
+  ARGS(ba_qk_norm_rope, 11); PRESENT(ba_qk_norm_rope); CTX; R(1, q); R(2, k); I(3, n); T(4, pos); P(5, wq); P(6, wk); F(7, eps); P(8, q_out); P(9, k_out);
   P(10, stream);
   CALL(p_ba_qk_norm_rope(ctx, q, q_stride, k, k_stride, n, pos, wq, wk, eps, q_out, k_out, stream));
 }
 static PyObject *m_qk_norm_rope_bwd(PyObject *self, PyObject *const *args, Py_ssize_t nargs) {
-  ARGS(ba_qk_norm_rope_bwd, 16); PRESENT(ba_qk_norm_rope_bwd); CTX; R(1, q); R(2, k); I(3, n); P(4, pos); P(5, wq); P(6, wk); F(7, eps); P(8, dyq); P(9, dyk);
+  ARGS(ba_qk_norm_rope_bwd, 16); PRESENT(ba_qk_norm_rope_bwd); CTX; R(1, q); R(2, k); I(3, n); T(4, pos); P(5, wq); P(6, wk); F(7, eps); P(8, dyq); P(9, dyk);
   R(10, dq); R(11, dk); P(12, dwq); P(13, dwk); I(14, type); P(15, stream);
   CALL(p_ba_qk_norm_rope_bwd(ctx, q, q_stride, k, k_stride, n, pos, wq, wk, eps, dyq, dyk, dq, dq_stride, dk, dk_stride, dwq, dwk, type, stream));
 }
 static PyObject *m_append_paged(PyObject *self, PyObject *const *args, Py_ssize_t nargs) {
-  ARGS(ba_append_paged, 17); PRESENT(ba_append_paged); CTX; R(1, q); R(2, k); R(3, v); I(4, n); P(5, pos); P(6, wq); P(7, wk); F(8, eps); P(9, cu);
-  P(10, start); I(11, n_seqs); P(12, q_out); P(13, kp); P(14, vp); PAGES(15, pages); P(16, stream);
+  ARGS(ba_append_paged, 17); PRESENT(ba_append_paged); CTX; R(1, q); R(2, k); R(3, v); I(4, n); T(5, pos); P(6, wq); P(7, wk); F(8, eps); T(9, cu);
+  T(10, start); I(11, n_seqs); P(12, q_out); P(13, kp); P(14, vp); PAGES(15, pages); P(16, stream);
   CALL(p_ba_append_paged(ctx, q, q_stride, k, k_stride, v, v_stride, n, pos, wq, wk, eps, cu, start, n_seqs, q_out, kp, vp, pages, stream));
 }
 static PyObject *m_shared_prefix_attend(PyObject *self, PyObject *const *args, Py_ssize_t nargs) {
@@ -252,5 +274,7 @@ PyMODINIT_FUNC PyInit_ba_marshal(void) {
   s_is_contiguous = PyUnicode_InternFromString("is_contiguous");
   s_stride = PyUnicode_InternFromString("stride");
   s_shape = PyUnicode_InternFromString("shape");
-  return s_data_ptr && s_is_contiguous && s_stride && s_shape ? PyModule_Create(&module) : NULL;
+  s_dtype = PyUnicode_InternFromString("dtype");
+  s_is_cuda = PyUnicode_InternFromString("is_cuda");
+  return s_data_ptr && s_is_contiguous && s_stride && s_shape && s_dtype && s_is_cuda ? PyModule_Create(&module) : NULL;
 }

@@ -56,3 +56,38 @@ def test_packed_rows_and_rows_of_a_fused_projection_reach_the_library(way, call,
         with pytest.raises(B.BaError) as e:
             call(**{name: x})
         assert e.value.status == B.BA_ERR_INVALID_ARG
+
+
+# ------------------------------------------------------------------ tables
+class _OnDevice:
+    """What the binding asks of a table on the device."""
+    is_cuda = True
+
+    def __init__(self, dtype=torch.int32):
+        self.dtype = dtype
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return ADDRESS
+
+
+TABLES = [(_norm, "pos"), (_norm_bwd, "pos"), (_append, "pos"), (_append, "seq_cu"), (_append, "seq_start")]
+
+
+@pytest.mark.parametrize("bad", [_OnDevice(torch.int64), _OnDevice(torch.float32), torch.arange(4), torch.arange(4, dtype=torch.int32),
+                                 torch.arange(4, dtype=torch.int32).numpy(), [0, 1, 2, 3]], ids=["int64", "float", "host int64", "host int32", "numpy", "list"])
+@pytest.mark.parametrize("call,name", TABLES, ids=lambda v: v if isinstance(v, str) else v.__name__)
+def test_tables_of_another_type_or_on_the_host_are_refused(way, call, name, bad):
+    """An int64 arange, torch's default, would be read as pairs of 32-bit positions, one on the host not at all."""
+    with pytest.raises(ValueError, match="int32 tensor"):
+        call(**{name: bad})
+
+
+@pytest.mark.parametrize("call,name", TABLES, ids=lambda v: v if isinstance(v, str) else v.__name__)
+def test_tables_on_the_device_and_addresses_reach_the_library(way, call, name):
+    for good in (_OnDevice(), ADDRESS, None):
+        with pytest.raises(B.BaError) as e:
+            call(**{name: good})
+        assert e.value.status == B.BA_ERR_INVALID_ARG
