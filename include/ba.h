@@ -244,8 +244,9 @@ ba_status ba_reencode_k(ba_ctx *ctx, const void *k_src, const int32_t *src_off, 
  * background of that kernel, and is complete when that kernel completes (stream order, as usual).
  * The job must not touch the tensors that attention call reads or writes.  One job can be queued
  * per context: queuing another, ba_flush() or ba_destroy() run a still-queued job as an ordinary
- * stand-alone launch.  Results are bit-identical to ba_reencode_k.  The queued job's arguments
- * (device pointers) must stay valid until it has run.
+ * stand-alone launch, and so do ba_qk_norm_rope, ba_append_paged and ba_shared_prefix_attend where the
+ * keys they are given lie in its k_dst (they leave any other job queued).  Results are bit-identical to
+ * ba_reencode_k.  The queued job's arguments (device pointers) must stay valid until it has run.
  */
 ba_status ba_reencode_k_deferred(ba_ctx *ctx, const void *k_src, const int32_t *src_off, int32_t n_src_rows,
                                  void *k_dst, const int32_t *cu, const int32_t *delta, int32_t n_blocks,

@@ -509,6 +509,13 @@ ba_status ba_block_prefill_bwd(ba_ctx *ctx, const void *q, const void *k, const 
 
 }  // extern "C"
 
+ba_status ba_flush_pending_into(ba_ctx *ctx, const void *p, size_t bytes, cudaStream_t stream) {
+  if (!ctx->has_pending) return BA_OK;
+  const uintptr_t dst = (uintptr_t)ctx->pending.dst, at = (uintptr_t)p;
+  if (dst >= at + bytes || at >= dst + (size_t)ctx->pending.n_rows * ctx->pending.row_vecs * 16) return BA_OK;
+  return ba_flush_pending(ctx, stream);
+}
+
 ba_status ba_check_pages(const ba_page_table *pg) {
   if (!pg || !pg->page_cu || !pg->page_idx) return BA_ERR_INVALID_ARG;
   if (pg->page_rows < 16 || pg->page_rows > 65536 || (pg->page_rows & (pg->page_rows - 1))) return BA_ERR_UNSUPPORTED;

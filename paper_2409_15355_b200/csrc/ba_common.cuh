@@ -172,6 +172,9 @@ ba_reencode_job ba_make_reencode_job(const ba_ctx *ctx, const void *k_src, const
 // Runs a pending deferred job as a stand-alone launch (no-op when nothing is pending).
 ba_status ba_flush_pending(ba_ctx *ctx, cudaStream_t stream);
 
+// The same for a pending job whose keys go anywhere into [p, p + bytes), which the call that asks is about to read.
+ba_status ba_flush_pending_into(ba_ctx *ctx, const void *p, size_t bytes, cudaStream_t stream);
+
 // Checks of a page table's host-side fields.
 ba_status ba_check_pages(const ba_page_table *pages);
 

@@ -492,6 +492,11 @@ int lay_out(const ba_ctx *ctx, NormParams &p, int ctas_a_sm, const bool (&there)
 
 template <bool kAppend>
 ba_status launch_norm_rope(ba_ctx *ctx, NormParams &p, const bool (&there)[3], cudaStream_t stream) {
+  if (there[kK]) {                                         // keys that a queued re-encoding is to write
+    const size_t row = (size_t)p.side[kK].heads * ctx->cfg.head_dim;
+    const ba_status st = ba_flush_pending_into(ctx, p.side[kK].x, ((size_t)(p.n_rows - 1) * p.side[kK].stride + row) * 2, stream);
+    if (st != BA_OK) return st;
+  }
   p.status = ctx->dev_status;
   memcpy(p.turns, ctx->turns, sizeof(p.turns));
   const int grid = lay_out(ctx, p, kFwdCtas, there);

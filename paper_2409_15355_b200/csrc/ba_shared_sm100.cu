@@ -1211,6 +1211,12 @@ ba_status ba_shared_prefix_attend(ba_ctx *ctx, const void *q, int32_t n_q_rows, 
   if (!ctx->workspace || ba_scratch_offset(ctx) + need + ctx->pending_table_bytes > ctx->workspace_bytes) return BA_ERR_WORKSPACE;
   if ((long long)n_q_rows * ctx->cfg.n_q_heads > INT32_MAX) return BA_ERR_SHAPE;
   BA_CUDA_TRY(cudaSetDevice(ctx->device));
+  const cudaStream_t cs = (cudaStream_t)stream;
+  const size_t kv_row = (size_t)ctx->cfg.n_kv_heads * D * 2;
+  st = ba_flush_pending_into(ctx, k_pool, kv_row * pages->n_pages * pages->page_rows, cs);
+  if (st == BA_OK && b->n_groups > 0)
+    st = ba_flush_pending_into(ctx, k_prefix, kv_row * (prefix_pages ? (size_t)prefix_pages->n_pages * prefix_pages->page_rows : n_prefix_rows), cs);
+  if (st != BA_OK) return st;
   auto lg_of = [](const ba_page_table *t) { int lg = 0; while ((1 << lg) < t->page_rows) ++lg; return lg; };
   SharedParams p = {};
   p.q = (const __nv_bfloat16 *)q; p.o = o; p.lse = lse; p.status = ctx->dev_status;
@@ -1244,7 +1250,6 @@ ba_status ba_shared_prefix_attend(ba_ctx *ctx, const void *q, int32_t n_q_rows, 
     if (!ba_tensor_map(ctx, &tkx, k_prefix, p.Hkv, prows, 1, pbox) || !ba_tensor_map(ctx, &tvx, v_prefix, p.Hkv, prows, 1, pbox)) return BA_ERR_CUDA;
   }
   const dim3 grid((unsigned)ctx->sm_count);
-  const cudaStream_t cs = (cudaStream_t)stream;
   // (16 requests over 32000 tokens: 512 rows of 35 results; 24 questions: 32600 rows of four)
   const long long rows_out = (long long)n_q_rows * p.Hq;
   const bool wide = rows_out <= 16384;                     // (5120 rows of seven results: 9.7 us with a warp a row, 15.3 with eight lanes)

@@ -156,3 +156,50 @@ def test_results_of_calls_in_close_succession():
     for key in ("q", "o", "dw"):
         assert not torch.equal(alone[0][key], alone[1][key])
     c.close()
+
+
+# ------------------------------------------------------------------ a queued re-encoding
+@pytest.mark.parametrize("reader", ["packed prefix", "pool of the prefix", "own pool", "append", "norm"])
+def test_a_queued_reencoding_is_run_before_its_keys_are_read(reader):
+    """The call that takes the queued job's k_dst finds the keys in it, without a ba_flush in between."""
+    shape = (8, 2, 128)
+    hq, hkv, d = shape
+    cfg = B.ba_config(*shape, 0, 1e4, 0.0, 0)
+    c = R.Context(*shape, 1e4, max_blocks=64, max_q_rows=64, workspace_bytes=B.ba_shared_prefix_bytes(cfg, 3, 1, 3) + (1 << 20))
+    rows, page_rows = 96, 16
+    k, v, q = bf16(rows, hkv, d, seed=1), bf16(rows, hkv, d, seed=2), bf16(3, hq, d, seed=3)
+    cu, delta = ints([0, 40, rows]), ints([0, 40])
+    tables = ints([0, 6]), ints([5, 3, 1, 0, 2, 4]), ints([0, 2, 4, 6]), ints([0, 3]), ints([0, 90]), ints([20, 30, 0]), ints([0] * rows), ints([0, rows])
+    whole, apart = B.make_page_table(page_rows, 6, *tables[:2]), B.make_page_table(page_rows, 6, tables[2], tables[1])
+    own = bf16(rows, hkv, d, seed=4)
+
+    def read(keys):
+        o, lse = torch.zeros(3, hq, d, device="cuda"), torch.zeros(3, hq, device="cuda")
+        shared = B.make_shared_batch(3, 1, tables[3], tables[4], None, tables[5])
+        if reader == "packed prefix":
+            B.ba_shared_prefix_attend(c.ctx, q, 3, keys, v, rows, None, own, v, apart, shared, o, lse, B.BA_OUT_F32)
+        elif reader == "pool of the prefix":
+            B.ba_shared_prefix_attend(c.ctx, q, 3, keys, v, 0, whole, own, v, apart, shared, o, lse, B.BA_OUT_F32)
+        elif reader == "own pool":
+            B.ba_shared_prefix_attend(c.ctx, q, 3, own, v, rows, None, keys, v, apart, shared, o, lse, B.BA_OUT_F32)
+        elif reader == "append":
+            pools = [torch.zeros(rows, hkv, d, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+            B.ba_append_paged(c.ctx, None, keys, v, rows, None, None, None, 0.0, tables[7], tables[6], 1, None, *pools, whole)
+            return pools
+        else:
+            out = torch.zeros(rows, hkv, d, dtype=torch.bfloat16, device="cuda")
+            B.ba_qk_norm_rope(c.ctx, None, keys, rows, None, None, None, 0.0, None, out)
+            return [out]
+        return [o, lse]
+
+    plain = torch.zeros_like(k)
+    B.ba_reencode_k(c.ctx, k, None, rows, plain, cu, delta, 2, rows)
+    want = read(plain)
+    queued = torch.zeros_like(k)
+    B.ba_reencode_k_deferred(c.ctx, k, None, rows, queued, cu, delta, 2, rows)
+    got = read(queued)
+    assert c.device_status() == B.BA_OK
+    assert torch.equal(queued, plain)
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+    c.close()
