@@ -495,7 +495,10 @@ typedef struct {
  * What lies behind the end of a prefix, a sequence or a list in pages or rows is never used and may hold any bits.  A page number outside
  * its pool counts as zeros and is reported (BA_ERR_INVALID_ARG).  Tables that do not fit together (a cumulative table that decreases
  * or leaves its range, a list of pages that begins below zero, a length below zero or above its list's pages) are reported the same way
- * and nothing is written; so is an amount of work beyond any launch (key tiles of 128 x KV heads x 256 query rows of all entries above six hundred million).
+ * and nothing is written; so is an amount of work beyond any launch.  It is counted for two kinds of entries (a prefix with the query rows
+ * of its group, a sequence with its own).  Those whose query rows x query heads a KV head are at most 16 count, for each KV head, a unit for
+ * every 128 keys and four more.  The others count, for each KV head and each 256 of these rows, three units for every 128 keys (two
+ * where 128 rows or fewer are left) and ten more.  Either sum may be up to 2 000 000 000, and an entry up to 2^31 - 257 keys long.
  * Keys, values and queries that are not finite act as in the formula: a row that sees a score which is NaN or +infinity is NaN, and so is its
  * log-sum-exp; a value that is NaN makes its column NaN.  (A value counts, with weight zero, for the rows of its sequence that come before
  * it as well: zero times NaN.  A key does not.)

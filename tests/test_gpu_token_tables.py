@@ -203,3 +203,59 @@ def test_a_queued_reencoding_is_run_before_its_keys_are_read(reader):
     for a, b in zip(got, want):
         assert torch.equal(a, b)
     c.close()
+
+
+# ------------------------------------------------------------------ pages outside the pool, on every path
+@pytest.mark.parametrize("questions", [[1, 2], [20, 3], [70, 60]], ids=["few rows", "a query tile", "two query tiles"])
+@pytest.mark.parametrize("which", ["own", "prefix"])
+@pytest.mark.parametrize("page_rows", [16, 64, 256])
+def test_pages_outside_the_pool_count_as_zeros_on_every_path(questions, which, page_rows):
+    shape = (4, 2, 64)
+    b = Batch(shape, [700], [0, 2], questions, [600, 300], page_rows, False, seed=13)
+    c = make_context(shape, b)
+    cu, idx = (b.keep if which == "own" else b.keep2)
+    pool = b.pool if which == "own" else b.kv_prefix
+    n_pages = pool[0].shape[0] // page_rows
+    nth = 1                                                    # the second page of the first list
+    zeros = [torch.cat([p, torch.zeros_like(p[:page_rows])]) for p in pool]
+    for bad in (-1, n_pages, 2 ** 31 - 1):
+        wrong = idx.clone()
+        wrong[nth] = bad
+        table = B.make_page_table(page_rows, n_pages, cu, wrong)
+        o, lse = torch.full((b.rows, 4, 64), 5.0, device="cuda"), torch.full((b.rows, 4), 6.0, device="cuda")
+        kept = b.table, b.prefix_table, b.pool, b.kv_prefix, b.idx, b.prefix_rows
+        if which == "own":
+            b.table = table
+        else:
+            b.prefix_table = table
+        b.call(c, o, lse, B.BA_OUT_F32)
+        assert c.device_status() == B.BA_ERR_INVALID_ARG
+        if which == "own":                                     # the reference reads the page from behind the pool, where zeros are
+            b.pool, b.idx = zeros, b.idx.copy()
+            b.idx[nth] = n_pages
+        else:
+            b.kv_prefix = zeros
+            b.prefix_rows = [[n_pages * page_rows + t % page_rows if t // page_rows == nth else r for t, r in enumerate(b.prefix_rows[0])]]
+        check_attention(b, o, lse, B.BA_OUT_F32, 0.125)
+        b.table, b.prefix_table, b.pool, b.kv_prefix, b.idx, b.prefix_rows = kept
+    c.close()
+
+
+# ------------------------------------------------------------------ more work than any launch takes
+@pytest.mark.parametrize("rows", [1, 3], ids=["few rows", "many rows"])
+@pytest.mark.parametrize("n_seqs,length", [(40, 2 ** 31 - 257), (15, 2 ** 31 - 257), (2, 2 ** 31 - 1)], ids=["past 32 bits", "past the limit", "one too long"])
+def test_more_work_than_a_launch_takes_is_reported(rows, n_seqs, length):
+    """Lists that are long by their tables alone.  Units are counted in 64 bits: the first sum is 5.4e9, which 32 bits would take for
+    1.1e9.  Nothing is looked up in the lists, and nothing is written."""
+    shape = (64, 8, 64)
+    cfg = B.ba_config(*shape, 0, 1e4, 0.0, 0)
+    n = n_seqs * rows
+    c = R.Context(*shape, 1e4, max_blocks=64, max_q_rows=64, workspace_bytes=B.ba_shared_prefix_bytes(cfg, n_seqs, 0, n))
+    pool = [torch.zeros(65536, 8, 64, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    page_cu, page_idx, own, q_cu = ints(32768 * s for s in range(n_seqs + 1)), ints([0] * 64), ints([length] * n_seqs), ints(range(0, n + 1, rows))
+    o, lse = torch.full((n, 64, 64), 5.0, device="cuda"), torch.full((n, 64), 6.0, device="cuda")
+    B.ba_shared_prefix_attend(c.ctx, bf16(n, 64, 64, seed=1), n, None, None, 0, None, *pool, B.make_page_table(65536, 1, page_cu, page_idx),
+                              B.make_shared_batch(n_seqs, 0, None, None, q_cu, own), o, lse, B.BA_OUT_F32)
+    assert c.device_status() == B.BA_ERR_INVALID_ARG
+    assert (o == 5).all() and (lse == 6).all()
+    c.close()
