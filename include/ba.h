@@ -443,7 +443,8 @@ ba_status ba_qk_norm_rope(ba_ctx *ctx, const void *q, int64_t q_stride, const vo
  *   dq, dk       rows `dq_stride`, `dk_stride` elements apart (0: packed; else a multiple of 16 bytes); may be dy_q, dy_k themselves where packed
  *   dw_q, dw_k   fp32 [head_dim], written (not added to); given exactly where w_q, w_k are.  Zero for n_rows = 0.
  *   grad_dtype   type of dy_q, dy_k, dq and dk
- * Uses up to 592 * 8 * head_dim bytes of workspace when there is a norm (ba_workspace_bytes() counts them).  No atomics: results are run-to-run identical.
+ * dq, dk overlap no input but these.  Uses (2 x SMs + 2) * 4 * head_dim bytes of workspace when there is a norm (ba_workspace_bytes() counts
+ * them).  No atomics: results are run-to-run identical.
  */
 ba_status ba_qk_norm_rope_bwd(ba_ctx *ctx, const void *q, int64_t q_stride, const void *k, int64_t k_stride, int32_t n_rows,
                               const int32_t *pos, const void *w_q, const void *w_k, float eps, const void *dy_q, const void *dy_k,

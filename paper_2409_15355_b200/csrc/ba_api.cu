@@ -109,7 +109,7 @@ ba_status ba_workspace_bytes(const ba_config *cfg, int32_t max_blocks, int32_t m
   // the backward pass keeps dO . O (fp32 per row and query head) there
   size_t bwd = (size_t)max_q_rows * cfg->n_q_heads * sizeof(float);
   // gradients of the norms' weights: sums of every CTA
-  const size_t norms = (size_t)kBaNormGridMax * 2 * cfg->head_dim * sizeof(float);
+  const size_t norms = ba_norm_sums_bytes(kBaMostSms, cfg->head_dim);
   size_t scratch = table > splits ? table : splits;
   if (bwd > scratch) scratch = bwd;
   if (norms > scratch) scratch = norms;

@@ -178,8 +178,12 @@ ba_status ba_flush_pending_into(ba_ctx *ctx, const void *p, size_t bytes, cudaSt
 // Checks of a page table's host-side fields.
 ba_status ba_check_pages(const ba_page_table *pages);
 
-// CTAs whose sums of the norms' weight gradients the workspace has room for (four on each of 148 SMs).
-constexpr int kBaNormGridMax = 592;
+// SMs that a workspace sized without a device has room for.
+constexpr int kBaMostSms = 256;
+// CTAs an SM of the kernel of the norms' gradients (ba_norm_rope.cu), and the workspace for the sums that they leave: a side has a CTA at
+// least, and no call more than its sides' share of the SMs' room and two.
+constexpr int kBaNormBwdCtas = 2;
+static inline size_t ba_norm_sums_bytes(int sms, int head_dim) { return (size_t)(sms * kBaNormBwdCtas + 2) * head_dim * sizeof(float); }
 
 struct ba_attend_args {
   // queries / outputs: rows of the q packing (prompt packing for prefill, final packing for final attend)

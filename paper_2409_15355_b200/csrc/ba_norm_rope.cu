@@ -36,7 +36,7 @@ constexpr int kNormWarps = kNormThreads / 32;
 // Steps in flight a warp, and CTAs an SM: more of the one leave registers for fewer of the other.  131072 rows, us: 4 x 3 476, 4 x 4 482, 3 x 4 508,
 // 2 x 5 555, 8 x 2 629; gradients of 32768 rows: 4 x 2 190, 2 x 2 221, 1 x 4 227, 2 x 3 254, 3 x 3 315.
 constexpr int kAhead = 4, kBwdAhead = 4;
-constexpr int kFwdCtas = 3, kBwdCtas = 2;
+constexpr int kFwdCtas = 3, kBwdCtas = kBaNormBwdCtas;
 
 // One side of a call: rows of `heads` heads, `stride` elements apart.
 struct NormSide {
@@ -570,8 +570,7 @@ ba_status ba_qk_norm_rope_bwd(ba_ctx *ctx, const void *q, int64_t q_stride, cons
   if ((dq && dq == dy_q && dq_stride != q_row) || (dk && dk == dy_k && dk_stride != k_row)) return BA_ERR_INVALID_ARG;
   const bool sums = w_q || w_k;
   if (n_rows == 0 && !sums) return BA_OK;
-  // (a side has a CTA at least, and no call more than its share of the SMs' room and two)
-  const size_t need = sums ? (size_t)(ctx->sm_count * kBwdCtas + 2) * D * sizeof(float) : 0;
+  const size_t need = sums ? ba_norm_sums_bytes(ctx->sm_count, D) : 0;
   if (sums && (!ctx->workspace || ba_scratch_offset(ctx) + need + ctx->pending_table_bytes > ctx->workspace_bytes)) return BA_ERR_WORKSPACE;
   BA_CUDA_TRY(cudaSetDevice(ctx->device));
   const cudaStream_t cs = (cudaStream_t)stream;

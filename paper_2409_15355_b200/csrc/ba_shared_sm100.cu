@@ -13,7 +13,7 @@
 // laid out on the device from the caller's tables by every CTA for itself: the lengths of a captured launch change from replay to replay.
 //
 // A CTA has 384 threads, one CTA runs on an SM.
-// Few rows: warp 8 asks the copy engine for key and value tiles (a ring of stages, one box per page); warps 0-7 take 16 keys of a tile
+// Few rows: warps 8 and 9 ask the copy engine for key and value tiles (a ring of stages for both, one box per page); warps 0-7 take 16 keys of a tile
 // each, with mma.sync on operands from shared memory: S = Q K^T, softmax with maxima and sums of the warp's own keys, O += P V with P from
 // registers.  The warps share nothing until the end of a piece, where their maxima, sums and accumulators are merged.
 // Many rows: tcgen05 with accumulators in tensor memory, warps 0-3 and 4-7 softmax (a thread a row), warps 8 and 10 copy keys
@@ -50,7 +50,6 @@ constexpr int kThreads = 32 * kWarps + 128;
 constexpr int kConsumerRegs = 224, kCopyRegs = 56;
 constexpr int kMaxEntries = BA_SHARED_MAX;
 constexpr int kSoftmaxRegs = 208, kServiceRegs = 88;     // of CTAs for many rows: 256 * 208 + 128 * 88
-// What a key tile costs, to share out the CTAs: two query tiles, one, and few rows (cycles / 1000).
 // Units of the streams.  A key tile counts for one in the stream of few rows and, in the other, for three with two query tiles and two with
 // one; an item counts besides for what begins and ends it (queries, the pipeline's filling, the rows' way out).
 constexpr int kTileFew = 1, kTilePair = 3, kTileSolo = 2, kFrontFew = 4, kFrontMany = 10;
@@ -1163,7 +1162,6 @@ bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) ==
 // Rows of partial results: four for every (query row, head), and kManyRows a CTA.
 long long part_rows(const ba_config &c, int n_q_rows, int n_ctas) { return 4ll * n_q_rows * c.n_q_heads + (long long)n_ctas * kManyRows; }
 size_t meta_bytes(int n_entries) { return ba_align_up((size_t)(n_entries + 1) * sizeof(int4), 256); }
-constexpr int kMostCtas = 256;        // sizing without a device
 
 }  // namespace
 
@@ -1182,7 +1180,7 @@ ba_status ba_shared_prefix_bytes(const ba_config *cfg, int32_t batch, int32_t n_
   if (!bytes || batch < 1 || n_groups < 0 || n_q_rows < 0) return BA_ERR_INVALID_ARG;
   if ((long long)batch + n_groups > BA_SHARED_MAX) return BA_ERR_UNSUPPORTED;
   *bytes = ba_scratch_offset(nullptr) + meta_bytes(batch + n_groups) +
-           (size_t)part_rows(*cfg, n_q_rows, kMostCtas) * (cfg->head_dim + 1) * sizeof(float) + 256;
+           (size_t)part_rows(*cfg, n_q_rows, kBaMostSms) * (cfg->head_dim + 1) * sizeof(float) + 256;
   return BA_OK;
 }
 

@@ -259,3 +259,21 @@ def test_more_work_than_a_launch_takes_is_reported(rows, n_seqs, length):
     assert c.device_status() == B.BA_ERR_INVALID_ARG
     assert (o == 5).all() and (lse == 6).all()
     c.close()
+
+
+def test_gradients_fit_the_workspace_that_is_asked_for():
+    """The smallest that ba_workspace_bytes() gives, and rows enough for every CTA: sums of both sides at once."""
+    for shape in ((32, 8, 128), (64, 1, 64), (1, 1, 128)):
+        hq, hkv, d = shape
+        rows, cfg = 6000, B.ba_config(*shape, 0, 1e4, 0.0, 0)
+        ctx = B.ba_create(cfg, 0, B.ba_workspace_bytes(cfg, 1, 0))
+        q, k, dy = bf16(rows, hq, d, seed=1), bf16(rows, hkv, d, seed=2), bf16(rows, hq, d, seed=3)
+        w, dw = bf16(d, seed=4), torch.full((2, d), float("nan"), device="cuda")
+        B.ba_qk_norm_rope_bwd(ctx, q, k, rows, None, w, w, 1e-6, dy, dy[:, :hkv].contiguous(), torch.empty_like(q), torch.empty_like(k), dw[0], dw[1],
+                              B.BA_OUT_BF16)
+        assert B.ba_last_device_status(ctx) == B.BA_OK
+        for got, x, g in ((dw[0], q, dy), (dw[1], k, dy[:, :hkv])):
+            xn = x.double() / torch.sqrt(x.double().square().mean(-1, keepdim=True) + 1e-6)
+            want, terms = (g.double() * xn).sum((0, 1)), (g.double() * xn).abs().sum((0, 1))
+            assert ((got.double() - want).abs() <= 2e-5 * terms).all()
+        B.ba_destroy(ctx)
