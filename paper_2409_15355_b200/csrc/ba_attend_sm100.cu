@@ -1375,9 +1375,9 @@ ba_attend_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_
       }
       if (ok && !(solo && t == 1)) {
         tc_fence_after();
-        const float inv_l = l > 0.f ? 1.f / l : 0.f, inv = weight * inv_l;
+        const float inv_l = l != 0.f ? 1.f / l : 0.f, inv = weight * inv_l;       // (a NaN goes through)
         inv1 *= inv_l;
-        const float lse_val = l > 0.f ? (m_used * sl + log2f(l)) * 0.6931471805599453f : -INFINITY;
+        const float lse_val = l != 0.f ? (m_used * sl + log2f(l)) * 0.6931471805599453f : -INFINITY;
         const bool partial = !kClustered && e.split >= 0;
         // Rows leave through shared memory -- the warp's quarter of the entry's own query tile, which every product has
         // read by now -- so that a store instruction writes whole rows: stores straight from the row each thread owns touch
