@@ -277,3 +277,78 @@ def test_gradients_fit_the_workspace_that_is_asked_for():
             want, terms = (g.double() * xn).sum((0, 1)), (g.double() * xn).abs().sum((0, 1))
             assert ((got.double() - want).abs() <= 2e-5 * terms).all()
         B.ba_destroy(ctx)
+
+
+# ------------------------------------------------------------------ what the documentation allows at its ends
+WIDE = {"one token": ([40], [0, 1], [1], [30], 16, False), "one token alone": ([], [0], [1], [300], 16, True),
+        "questions": ([500], [0, 2], [3, 1], [140, 5], 64, True), "cut": ([4000], [0, 2], [2, 1], [900, 5], 16, False)}
+
+
+@pytest.mark.parametrize("shape", [(160, 1, 64), (256, 2, 128), (129, 1, 128), (128, 1, 64), (64, 1, 128), (17, 1, 64), (16, 1, 128)], ids=str)
+@pytest.mark.parametrize("name", list(WIDE))
+def test_many_query_heads_a_kv_head(shape, name):
+    b = Batch(shape, *WIDE[name], seed=21)
+    c = make_context(shape, b)
+    o, lse = torch.full((b.rows, *shape[::2]), 5.0, device="cuda"), torch.full((b.rows, shape[0]), 6.0, device="cuda")
+    b.call(c, o, lse, B.BA_OUT_F32)
+    assert c.device_status() == B.BA_OK
+    check_attention(b, o, lse, B.BA_OUT_F32, shape[2] ** -0.5)
+    c.close()
+
+
+@pytest.mark.parametrize("name,case", {"most entries": ([3, 0, 40, 7, 130], [0, 9, 700, 701, 1500, 2043], [1] * 2043, [(5 * i) % 23 for i in range(2043)], 16, False),
+                                       "a group each": ([(7 * i) % 150 for i in range(500)], list(range(501)), [1 + i % 2 for i in range(500)], [2 + i % 30 for i in range(500)],
+                                                        16, True),
+                                       "a group each, many rows": ([(37 * i) % 400 for i in range(30)], list(range(31)), [9 + i for i in range(30)], [i * 20 for i in range(30)],
+                                                                   32, False)}.items())
+def test_as_many_sequences_and_groups_as_there_can_be(name, case):
+    shape = (4, 2, 64)
+    b = Batch(shape, *case, seed=22)
+    c = make_context(shape, b)
+    o, lse = torch.full((b.rows, 4, 64), 5.0, device="cuda"), torch.full((b.rows, 4), 6.0, device="cuda")
+    b.call(c, o, lse, B.BA_OUT_F32)
+    assert c.device_status() == B.BA_OK
+    check_attention(b, o, lse, B.BA_OUT_F32, 0.125)
+    c.close()
+
+
+@pytest.mark.parametrize("packed", [True, False])
+@pytest.mark.parametrize("questions", [[1, 2, 1, 1], [20, 3, 1, 70]], ids=["few rows", "many rows"])
+def test_tables_that_do_not_begin_at_zero(packed, questions):
+    """Cumulative tables that are windows of longer ones: query rows in front of the first sequence, prefixes behind others, a first group that begins
+    later, lists of pages behind others."""
+    shape = (4, 2, 64)
+    b = Batch(shape, [200, 77], [1, 2, 4], questions, [90, 30, 5, 140], 16, packed, seed=23)
+    c = R.Context(*shape, 1e4, max_blocks=64, max_q_rows=64, workspace_bytes=B.ba_shared_prefix_bytes(B.ba_config(*shape, 0, 1e4, 0.0, 0), 4, 2, b.rows + 5))
+    shift = lambda t, n: (t + n).contiguous()
+    q = torch.cat([torch.full((5, 4, 64), float("nan"), dtype=torch.bfloat16, device="cuda"), b.q])
+    group_cu, prefix_cu, q_cu, own = b.tables
+    q_cu = shift(ints(b.q_cu), 5)
+    before = torch.full((37, 2, 64), float("nan"), dtype=torch.bfloat16, device="cuda")
+    prefix = [torch.cat([before, p]) for p in b.kv_prefix] if packed else b.kv_prefix
+    prefix_cu = shift(prefix_cu, 37)
+    listed = lambda keep, n: (shift(keep[0], 3), torch.cat([torch.full((3,), n, dtype=torch.int32, device="cuda"), keep[1]]))   # (three pages that are not there)
+    own_lists, lists = listed(b.keep, b.n_pages), None if packed else listed(b.keep2, prefix[0].shape[0] // 16)
+    o, lse = torch.full((b.rows + 5, 4, 64), 5.0, device="cuda"), torch.full((b.rows + 5, 4), 6.0, device="cuda")
+    B.ba_shared_prefix_attend(c.ctx, q, b.rows + 5, *prefix, b.n_prefix + 37, None if packed else B.make_page_table(16, prefix[0].shape[0] // 16, *lists), *b.pool,
+                              B.make_page_table(16, b.n_pages, *own_lists), B.make_shared_batch(4, 2, group_cu, prefix_cu, q_cu, own), o, lse, B.BA_OUT_F32)
+    assert c.device_status() == B.BA_OK
+    assert (o[:5] == 5).all() and (lse[:5] == 6).all()
+    check_attention(b, o[5:], lse[5:], B.BA_OUT_F32, 0.125)
+    c.close()
+
+
+def test_append_with_rows_in_front_of_the_first_sequence():
+    c = context((4, 2, 64))
+    q, k, v = bf16(9, 4, 64, seed=3), bf16(9, 2, 64, seed=1), bf16(9, 2, 64, seed=2)
+    pools = [torch.full((64, 2, 64), 9.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    q_out, tables = torch.full_like(q, 3.0), (ints([2, 5, 5, 8]), ints([14, 0, 1]), ints([1, 3, 3, 4]), ints([99, 2, 0, 3]))
+    B.ba_append_paged(c.ctx, q, k, v, 9, None, None, None, 0.0, *tables[:2], 3, q_out, *pools, B.make_page_table(16, 4, *tables[2:]))
+    assert c.device_status() == B.BA_OK
+    assert torch.equal(q_out[2:8], q[2:8]) and (q_out[:2] == 3).all() and (q_out[8:] == 3).all()
+    at = [32 + 14, 32 + 15, 0, 48 + 1, 48 + 2, 48 + 3]           # (rows 2, 3, 4 of list 0 over its pages 2 and 0; rows 5, 6, 7 of list 2 on page 3)
+    for p, x in zip(pools, (k, v)):
+        assert torch.equal(p[at], x[2:8])
+        p[at] = 9.0
+        assert (p == 9).all()
+    c.close()
