@@ -51,9 +51,12 @@ constexpr int kConsumerRegs = 224, kCopyRegs = 56;
 constexpr int kMaxEntries = BA_SHARED_MAX;
 constexpr int kSoftmaxRegs = 208, kServiceRegs = 88;     // of CTAs for many rows: 256 * 208 + 128 * 88
 // Units of the streams.  A key tile counts for one in the stream of few rows and, in the other, for three with two query tiles and two with
-// one; an item counts besides for what begins and ends it (queries, the pipeline's filling, the rows' way out).
+// one; an item counts besides for what begins and ends it (queries, the pipeline's filling, the rows' way out).  Measured, us: few rows' 1, 4, 8
+// units: 16 requests over 32000 tokens 61.7, 49.1, 48.7, 160 requests in seven groups 200, 192, 211, 64 apart 180, 177, 181; many rows' 3, 10, 20:
+// 24 questions over 16384 tokens 451, 308, 312, the seven groups 197, 192, 193.
 constexpr int kTileFew = 1, kTilePair = 3, kTileSolo = 2, kFrontFew = 4, kFrontMany = 10;
-// What a unit costs, to share out the CTAs between the streams.
+// What a unit costs, to share out the CTAs between the streams.  2, 3, 4.5 for few rows against 2: the 16 requests 53.5, 49.1, 48.5 us, the seven
+// groups 210, 192, 232, the others, of one kind nearly alone, the same.
 constexpr float kCostFew = 3.f, kCostMany = 2.f;
 constexpr long long kMostUnits = 2000000000;               // of a stream: places in it are 32 bits
 constexpr float kRescale = 8.f;       // O is rescaled when a maximum grows by more than 2^8: exact in real arithmetic, values stay bounded
@@ -1007,7 +1010,7 @@ ba_shared_attend_kernel(const __grid_constant__ CUtensorMap tmap_kx, const __gri
 
 // The partial results of every (row, head): those of its group's prefix and of its own rows, weighted by their denominators.  What a row
 // waits for is a chain of look-ups, so rows go side by side: eight lanes a row (32600 rows: 34 us with a warp each), or, with few rows,
-// whose long prefixes leave many results, a warp or several.
+// whose long prefixes leave many results, a warp or four (the figures are at the launch).
 template <int D, int kL>
 __global__ void __launch_bounds__(256)
 ba_shared_merge_kernel(const __grid_constant__ SharedParams p, int warps_a_row) {
@@ -1248,10 +1251,14 @@ ba_status ba_shared_prefix_attend(ba_ctx *ctx, const void *q, int32_t n_q_rows, 
     if (!ba_tensor_map(ctx, &tkx, k_prefix, p.Hkv, prows, 1, pbox) || !ba_tensor_map(ctx, &tvx, v_prefix, p.Hkv, prows, 1, pbox)) return BA_ERR_CUDA;
   }
   const dim3 grid((unsigned)ctx->sm_count);
-  // (16 requests over 32000 tokens: 512 rows of 35 results; 24 questions: 32600 rows of four)
+  // How many lanes a row gets in the merge: what decides is rows x results, but results follow from lengths that the host does not read.  Calls of
+  // 32 heads over a shared prefix of 2000 / 32000 keys, us with 8 lanes, a warp, four warps a row: 512 rows 33.2, 24.4, 22.8 / 86.0, 50.1, 46.1;
+  // 1024 rows 32.1, 27.4, 26.5 / 87.7, 55.0, 53.5; 2048 rows 38.5, 36.0, 39.7 / 86.9, 69.5, 72.5; 4096 rows 49.8, 49.1, 58.8 / 118, 132, 134;
+  // 6144 rows 77.6, 75.5, 91.6 / 162, 182, 202; 8192 rows 88.4, 95.8, 111 / 202, 230, 262.  Without a prefix a warp a row is as good or better up
+  // to 6144 rows (300 keys each: 2048 rows 34.0, 32.3, 33.9; 6144 rows 78.2, 76.9, 83.6; 12288 rows 140.4, 140.9, 154.7).
   const long long rows_out = (long long)n_q_rows * p.Hq;
-  const bool wide = rows_out <= 16384;                     // (5120 rows of seven results: 9.7 us with a warp a row, 15.3 with eight lanes)
-  const int warps_a_row = rows_out <= 4096 ? 4 : 1;
+  const bool wide = rows_out <= 6144;
+  const int warps_a_row = rows_out <= 1024 ? 4 : 1;
   const unsigned merge = (unsigned)((rows_out * warps_a_row * (wide ? 32 : 8) + 255) / 256);
   if (D == 128) {
     BA_CUDA_TRY(ba_launch(ba_shared_attend_kernel<128>, grid, kThreads, SharedLayout<128>::kBytes, cs, true, tkx, tvx, tk, tv, tq, p));
