@@ -429,7 +429,7 @@ ba_status ba_final_attend_fused_paged(ba_ctx *ctx, const void *q_f, const void *
  *   pos          device int32 [n_rows], any value, or NULL: position 0 throughout, which rotates nothing
  *   w_q, w_k     bf16 [head_dim], 16-byte aligned, shared by the heads; NULL: that side is rotated only
  *   eps          not negative; ignored when both weights are NULL
- *   q_out, k_out bf16 packed [n_rows, heads, head_dim]; may be q, k themselves where those are packed, must not overlap them otherwise
+ *   q_out, k_out bf16 packed [n_rows, heads, head_dim]; may be q, k themselves where those are packed, must not overlap them or one another otherwise
  */
 ba_status ba_qk_norm_rope(ba_ctx *ctx, const void *q, int64_t q_stride, const void *k, int64_t k_stride, int32_t n_rows,
                           const int32_t *pos, const void *w_q, const void *w_k, float eps, void *q_out, void *k_out, void *stream);
@@ -440,11 +440,12 @@ ba_status ba_qk_norm_rope(ba_ctx *ctx, const void *q, int64_t q_stride, const vo
  *   q, k, pos, w_q, w_k, eps   what the forward call was given (q, k are not read, and may be NULL, where there is no norm)
  *   dy_q, dy_k   packed [n_rows, heads, head_dim]: gradients with respect to q_out, k_out (the dq, dk of ba_block_prefill_bwd); NULL
  *                with its output: that side is left out
- *   dq, dk       rows `dq_stride`, `dk_stride` elements apart (0: packed; else a multiple of 16 bytes); may be dy_q, dy_k themselves where packed
- *   dw_q, dw_k   fp32 [head_dim], written (not added to); given exactly where w_q, w_k are.  Zero for n_rows = 0.
+ *   dq, dk       rows `dq_stride`, `dk_stride` elements apart (0: packed; else a multiple of 16 bytes); may be dy_q, dy_k themselves where packed, or bf16
+ *                q, k themselves with the same strides; overlap nothing else
+ *   dw_q, dw_k   fp32 [head_dim], written (not added to), apart from one another even where w_q is w_k; given exactly where w_q, w_k are.  Zero
+ *                for n_rows = 0.
  *   grad_dtype   type of dy_q, dy_k, dq and dk
- * dq, dk overlap no input but these.  Uses (2 x SMs + 2) * 4 * head_dim bytes of workspace when there is a norm (ba_workspace_bytes() counts
- * them).  No atomics: results are run-to-run identical.
+ * Uses (2 x SMs + 2) * 4 * head_dim bytes of workspace when there is a norm (ba_workspace_bytes() counts them).  No atomics: results are run-to-run identical.
  */
 ba_status ba_qk_norm_rope_bwd(ba_ctx *ctx, const void *q, int64_t q_stride, const void *k, int64_t k_stride, int32_t n_rows,
                               const int32_t *pos, const void *w_q, const void *w_k, float eps, const void *dy_q, const void *dy_k,
@@ -460,7 +461,7 @@ ba_status ba_qk_norm_rope_bwd(ba_ctx *ctx, const void *q, int64_t q_stride, cons
  *                (n_seqs = n_rows, else BA_ERR_SHAPE).  Rows outside all sequences (padding) are left alone in every output.
  *   seq_start    device int32 [n_seqs]: the place in list s of pages that the sequence's first row goes to (its rows so far)
  *   pages        lists page_cu[s] .. of the sequences in the pools (ba_page_table, with sequences for blocks)
- *   k_pool, v_pool  bf16 [n_pages * page_rows, n_kv_heads, head_dim]; q, k, v do not overlap them
+ *   k_pool, v_pool  bf16 [n_pages * page_rows, n_kv_heads, head_dim]; q, k, v, q_out do not overlap them, nor q_out k, v
  * A row whose place has no page in its list (a list with page_cu[s] below zero has none), or a page outside the pool, is not written to
  * the pools and reported through ba_last_device_status() as BA_ERR_INVALID_ARG; its query is still written.  Two rows must not go to the same place.
  */

@@ -519,6 +519,7 @@ ba_status ba_qk_norm_rope(ba_ctx *ctx, const void *q, int64_t q_stride, const vo
   if ((q && !side_ok(q, &q_stride, q_row, 8)) || (k && !side_ok(k, &k_stride, k_row, 8))) return BA_ERR_INVALID_ARG;
   if (!aligned16(q_out) || !aligned16(k_out) || !aligned16(w_q) || !aligned16(w_k) || !eps_ok(eps, w_q, w_k)) return BA_ERR_INVALID_ARG;
   if ((q && q == q_out && q_stride != q_row) || (k && k == k_out && k_stride != k_row)) return BA_ERR_INVALID_ARG;
+  if (q && k && (q_out == k_out || q_out == k || k_out == q)) return BA_ERR_INVALID_ARG;       // (the sides run side by side)
   if (n_rows == 0) return BA_OK;
   BA_CUDA_TRY(cudaSetDevice(ctx->device));
   NormParams p = {};
@@ -540,6 +541,7 @@ ba_status ba_append_paged(ba_ctx *ctx, const void *q, int64_t q_stride, const vo
   if (!aligned16(q_out) || !aligned16(k_pool) || !aligned16(v_pool) || !aligned16(w_q) || !aligned16(w_k) || !eps_ok(eps, w_q, w_k))
     return BA_ERR_INVALID_ARG;
   if (k == k_pool || v == v_pool || k_pool == v_pool || (q && q == q_out && q_stride != q_row)) return BA_ERR_INVALID_ARG;
+  if (q && (q_out == k_pool || q_out == v_pool || q_out == k || q_out == v)) return BA_ERR_INVALID_ARG;
   if (!seq_cu && n_seqs != n_rows) return BA_ERR_SHAPE;
   if (n_rows == 0 || n_seqs == 0) return BA_OK;
   BA_CUDA_TRY(cudaSetDevice(ctx->device));
@@ -568,10 +570,15 @@ ba_status ba_qk_norm_rope_bwd(ba_ctx *ctx, const void *q, int64_t q_stride, cons
   if (!aligned16(dy_q) || !aligned16(dy_k) || !aligned16(w_q) || !aligned16(w_k) || !eps_ok(eps, w_q, w_k)) return BA_ERR_INVALID_ARG;
   if (!w_q != !dw_q || !w_k != !dw_k) return BA_ERR_INVALID_ARG;
   if ((dq && dq == dy_q && dq_stride != q_row) || (dk && dk == dy_k && dk_stride != k_row)) return BA_ERR_INVALID_ARG;
+  // the place of the inputs, too, if they lie row on row and value on value
+  const bool wide = grad_dtype == BA_OUT_F32;
+  if ((w_q && dq == q && (wide || dq_stride != q_stride)) || (w_k && dk == k && (wide || dk_stride != k_stride))) return BA_ERR_INVALID_ARG;
+  if (dq && dk && (dq == dk || dq == dy_k || dk == dy_q || (w_q && dk == q) || (w_k && dq == k))) return BA_ERR_INVALID_ARG;
   const bool sums = w_q || w_k;
   if (n_rows == 0 && !sums) return BA_OK;
   const size_t need = sums ? ba_norm_sums_bytes(ctx->sm_count, D) : 0;
   if (sums && (!ctx->workspace || ba_scratch_offset(ctx) + need + ctx->pending_table_bytes > ctx->workspace_bytes)) return BA_ERR_WORKSPACE;
+  if (dw_q && dw_q == dw_k) return BA_ERR_INVALID_ARG;
   BA_CUDA_TRY(cudaSetDevice(ctx->device));
   const cudaStream_t cs = (cudaStream_t)stream;
   NormParams p = {};

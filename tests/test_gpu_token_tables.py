@@ -352,3 +352,43 @@ def test_append_with_rows_in_front_of_the_first_sequence():
         p[at] = 9.0
         assert (p == 9).all()
     c.close()
+
+
+# ------------------------------------------------------------------ outputs in one another's place
+def test_outputs_in_the_place_of_others_are_refused():
+    """The sides of a call run side by side: an output of one in the place of what the other reads or writes has no defined contents."""
+    c = context((4, 4, 64))
+    n = 4
+    q, k, v, oq, ok, dyq, dyk = (bf16(n, 4, 64, seed=s) for s in range(7))
+    w, dw = bf16(64, seed=9), torch.zeros(2, 64, device="cuda")
+    pools, start = [torch.zeros(64, 4, 64, dtype=torch.bfloat16, device="cuda") for _ in range(2)], ints([0] * n)
+    table, keep = (lambda cu, idx: (B.make_page_table(16, 4, cu, idx), (cu, idx)))(ints(range(n + 1)), ints(range(n)))
+    before = c.launches()
+
+    def refused(call):
+        with pytest.raises(B.BaError) as e:
+            call()
+        assert e.value.status == B.BA_ERR_INVALID_ARG
+    norm = lambda a, b: lambda: B.ba_qk_norm_rope(c.ctx, q, k, n, None, w, w, 1e-6, a, b)
+    for a, b in ((oq, oq), (k, ok), (oq, q), (k, q)):
+        refused(norm(a, b))
+    bwd = lambda dq, dk, x=dw[0], y=dw[1], kind=B.BA_OUT_BF16: lambda: B.ba_qk_norm_rope_bwd(c.ctx, q, k, n, None, w, w, 1e-6, dyq, dyk, dq, dk, x, y, kind)
+    for a, b in ((oq, oq), (dyk, ok), (oq, dyq), (k, ok), (oq, q)):
+        refused(bwd(a, b))
+    refused(bwd(oq, ok, dw[0], dw[0]))
+    wide = torch.zeros(n, 8, 64, dtype=torch.bfloat16, device="cuda")
+    refused(lambda: B.ba_qk_norm_rope_bwd(c.ctx, wide[:, :4], None, n, None, w, None, 1e-6, dyq, None, wide.view(2 * n, 4, 64)[:n], None, dw[0], None, B.BA_OUT_BF16))
+    refused(lambda: B.ba_qk_norm_rope_bwd(c.ctx, q, None, n, None, w, None, 1e-6, torch.zeros(n, 4, 64, device="cuda"), None, q.data_ptr(), None, dw[0], None,
+                                          B.BA_OUT_F32))
+    for out in (pools[0], pools[1], k, v):
+        refused(lambda: B.ba_append_paged(c.ctx, q, k, v, n, None, None, None, 0.0, None, start, n, out, *pools, table))
+    assert c.launches() == before
+    # what stays allowed: gradients in the place of the inputs
+    norm(oq, ok)()
+    bwd(oq, ok)()
+    dws = dw.clone()
+    x, y = q.clone(), k.clone()
+    B.ba_qk_norm_rope_bwd(c.ctx, x, y, n, None, w, w, 1e-6, dyq, dyk, x, y, dw[0], dw[1], B.BA_OUT_BF16)
+    assert torch.equal(x, oq) and torch.equal(y, ok) and torch.equal(dw, dws)
+    assert c.device_status() == B.BA_OK
+    c.close()
