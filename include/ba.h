@@ -504,6 +504,8 @@ typedef struct {
  * Keys, values and queries that are not finite act as in the formula: a row that sees a score which is NaN or +infinity is NaN, and so is its
  * log-sum-exp; a value that is NaN makes its column NaN.  (A value counts, with weight zero, for the rows of its sequence that come before
  * it as well: zero times NaN.  A key does not.)
+ * The softmax's weights are rounded to bf16 for the product with the values, whatever out_dtype is (2^-8 of a term at most; scores, maxima and sums are
+ * fp32), as in the library's other attention calls.
  * Uses ba_shared_prefix_bytes() bytes of workspace at most (to be given to ba_create(); BA_ERR_WORKSPACE otherwise); batch + n_groups is
  * at most BA_SHARED_MAX (BA_ERR_UNSUPPORTED).  No atomics: results are run-to-run identical.
  */
