@@ -426,7 +426,8 @@ ba_status ba_final_attend_fused_paged(ba_ctx *ctx, const void *q_f, const void *
  *   q, k         bf16 rows of [n_q_heads, head_dim] and [n_kv_heads, head_dim], `q_stride` and `k_stride` elements apart (0: packed; else
  *                a multiple of 8, not less than a row), so that both may lie in the one buffer of a fused projection.  Either may be
  *                NULL with its output: that side is left out.
- *   pos          device int32 [n_rows], any value, or NULL: position 0 throughout, which rotates nothing
+ *   pos          device int32 [n_rows], any value, or NULL: position 0 throughout, which rotates nothing (a value that is not finite still
+ *                reaches the other of its rotary pair: infinity times sin 0 is NaN)
  *   w_q, w_k     bf16 [head_dim], 16-byte aligned, shared by the heads; NULL: that side is rotated only
  *   eps          not negative; ignored when both weights are NULL
  *   q_out, k_out bf16 packed [n_rows, heads, head_dim]; may be q, k themselves where those are packed, must not overlap them or one another otherwise
